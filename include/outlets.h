@@ -314,6 +314,154 @@ int outlets_probe_release(outlets_ctx* ctx, int32_t n, const int32_t* slots);
  */
 int outlets_draft_distribution(outlets_ctx* ctx, int32_t n_req, float* p_out, void* stream);
 
+/* ------------------------------------------------------------ paged cache on the GPU
+ * Operators over a paged KV cache in the caller's device memory, in the
+ * library's layout (pages of 16 tokens).  Unlike the context's own cache,
+ * whose page tables the host allocator keeps, everything a call depends on
+ * is read on the GPU, so a decode step can be captured into a HIP graph once
+ * and replayed while the requests grow.  The calls allocate nothing and keep
+ * nothing; the arguments are checked on the host before anything is queued,
+ * and what only the device can see is reported in a device status word.
+ * Device work runs on `device` of the state or cache (the caller's current
+ * device is put back) and on `stream`, which must belong to it.  Calls that
+ * share a state, a cache or a workspace must be ordered on one stream, also
+ * when they are replayed from different graphs.
+ */
+
+/*
+ * Page tables kept on the GPU (the device counterpart of outlets_pager_*:
+ * the same allocation order, so the same tables).
+ *   free_bits [ceil(num_pages / 32)]: bit p % 32 of word p / 32 set = page p free.
+ *   page_table [max_slots, ceil(max_seq_len / 16)]: pages of each slot, -1 = none.
+ *   seq_len [max_slots]: cached tokens of each slot.
+ * num_pages <= (2^31 - 1) / 16; max_slots <= 131072 (else UNSUPPORTED).
+ */
+typedef struct outlets_page_state {
+    uint32_t* free_bits;
+    int32_t* page_table;
+    int32_t* seq_len;
+    int32_t num_pages;
+    int32_t max_slots;
+    int32_t max_seq_len;
+    int32_t device;
+} outlets_page_state;
+
+/* All pages free, all slots empty. */
+int outlets_pages_reset(const outlets_page_state* state, void* stream);
+
+/*
+ * Appends new_tokens[i] >= 0 tokens to slot slots[i], for prompts (empty
+ * slots) and steps alike, and lays out their rows: packed, requests in order,
+ * tokens in order.  slots, new_tokens [n_req] are device arrays; a slot of -1
+ * pads the batch (nothing is appended, whatever its token count).
+ * Pages: lowest free ids first, requests in argument order.
+ * Outputs (device):
+ *   cu_out [n_req + 1]: first row of each request, and the row count T;
+ *   slot_map_out, positions_out, row_slot_out [n_rows]: of each row, its
+ *     place in the cache (page * 16 + offset), its position in the request
+ *     and its slot; -1 in rows T .. n_rows - 1;
+ *   status_out [4]: 0 or an error code, T, pages taken, free pages left.
+ * Device errors, the whole call refused, the state unchanged, every row -1,
+ * cu_out all 0 and T = 0: a slot outside [-1, max_slots) or given twice, a
+ * negative count, a length above max_seq_len or a T above n_rows
+ * (INVALID_ARG); too few free pages (OUT_OF_PAGES).
+ * Host errors: null or negative arguments, workspace (INVALID_ARG); more than
+ * 2^20 requests or rows (UNSUPPORTED).
+ *   ws: outlets_pages_append_workspace(n_req, n_rows) bytes (may be 0),
+ *     16-byte aligned.
+ */
+int outlets_pages_append(const outlets_page_state* state, int32_t n_req, const int32_t* slots,
+                         const int32_t* new_tokens, int32_t n_rows, int32_t* cu_out, int32_t* slot_map_out,
+                         int32_t* positions_out, int32_t* row_slot_out, int32_t* status_out, void* ws,
+                         int64_t ws_bytes, void* stream);
+int64_t outlets_pages_append_workspace(int32_t n_req, int32_t n_rows);
+
+/*
+ * Empties slots (device [n]; -1 is skipped, an empty slot is a no-op) and
+ * frees their pages.  status_out [1] (device): 0, or INVALID_ARG with no
+ * change for a slot outside [-1, max_slots) or given twice.
+ */
+int outlets_pages_release(const outlets_page_state* state, int32_t n, const int32_t* slots, int32_t* status_out,
+                          void* stream);
+
+/*
+ * A cache: pools and page table (device).  A call needs only the parts that
+ * it reads or writes; the others may be NULL.
+ *   k_pool [num_pages, n_kv, 16, hd], v_pool [num_pages, n_kv, hd, 16]
+ *     (values transposed), block_keys [num_pages, n_kv, hd], all in `fmt`
+ *     (F32 or BF16) and 16-byte aligned; hd 64 or 128.
+ *   page_table [max_slots, max_pages].
+ */
+typedef struct outlets_kv_pages {
+    void* k_pool;
+    void* v_pool;
+    void* block_keys;
+    const int32_t* page_table;
+    int32_t fmt;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t num_pages;
+    int32_t max_slots;
+    int32_t max_pages;
+    int32_t device;
+} outlets_kv_pages;
+
+/*
+ * Writes keys and values of n_rows rows to their places (slot_map as
+ * outlets_pages_append gives it; an entry outside [0, 16 num_pages) writes
+ * nothing).  Row r of k starts at element r * k_stride and holds n_kv heads of
+ * hd; v likewise; any alignment.  With block_keys (not NULL), a row that is
+ * the last of its page also leaves the page's block key: the mean of its 16
+ * keys, summed in position order in 64 bits, rounded to 32 bits and to fmt.  Rows of one page that are
+ * written by one call must follow each other, in position order, and no
+ * place may be given twice (outlets_pages_append's rows are so).
+ */
+int outlets_cache_write(const outlets_kv_pages* cache, int32_t n_rows, const int32_t* slot_map, const void* k,
+                        int64_t k_stride, const void* v, int64_t v_stride, void* stream);
+
+/*
+ * The pages that each row's sparse attention reads, per KV head.  Row r
+ * (slot row_slot[r], position positions[r]) sees pages 0 .. positions[r] / 16.
+ * With at most top_k visible, all of them; otherwise the first `sink`, the
+ * last `local` (>= 1: the newest page has no block key yet) and, of the
+ * others, the top_k - sink - local with the largest score
+ *   s_b = max over the query heads h of the KV head of  q_h . block_key_b,
+ * summed in 64 bits; ties go to the lowest page, a NaN product of a head
+ * leaves that head out.
+ *   q: row r at element r * q_stride, n_q_heads (at most 16 per KV head) of hd;
+ *     any alignment.
+ *   sel_out (device) [n_rows, n_kv, top_k]: page indexes within the request,
+ *     ascending, -1 behind them.  A row with a negative slot or position, or
+ *     one outside the page table, sees no page.
+ *   ws: 16-byte aligned; outlets_block_select_workspace(cache, n_rows) bytes,
+ *     or fewer down to that of one row (the rows are then taken in parts).
+ *     Not needed where max_pages <= top_k.
+ */
+int outlets_block_select(const outlets_kv_pages* cache, int32_t n_rows, const int32_t* row_slot,
+                         const int32_t* positions, const void* q, int64_t q_stride, int32_t n_q_heads, int32_t top_k,
+                         int32_t sink, int32_t local, int32_t* sel_out, void* ws, int64_t ws_bytes, void* stream);
+int64_t outlets_block_select_workspace(const outlets_kv_pages* cache, int32_t n_rows);
+
+/*
+ * Attention of each row over the tokens of its selected pages up to its own
+ * position: softmax(q . k / sqrt(hd)) v, statistics in fp32.  Entries of
+ * `sel` that are no page the row sees (-1, above positions[r] / 16, not in
+ * the table) are skipped; an entry given twice counts twice; a row without
+ * tokens gives zeros.  What the pages hold behind the row's position is not
+ * used.
+ *   q as above, rows 16-byte aligned (else UNSUPPORTED).
+ *   gate (nullable): laid out like q with its own stride; output element x is
+ *     multiplied by sigmoid(gate x) (the attention output gate).
+ *   out: fmt, row r at element r * out_stride.
+ *   ws: outlets_block_attention_workspace(...) bytes (may be 0), 16-byte aligned.
+ */
+int outlets_block_attention(const outlets_kv_pages* cache, int32_t n_rows, const int32_t* row_slot,
+                            const int32_t* positions, const void* q, int64_t q_stride, int32_t n_q_heads,
+                            const int32_t* sel, int32_t top_k, const void* gate, int64_t gate_stride, void* out,
+                            int64_t out_stride, void* ws, int64_t ws_bytes, void* stream);
+int64_t outlets_block_attention_workspace(const outlets_kv_pages* cache, int32_t n_rows, int32_t n_q_heads,
+                                          int32_t top_k);
+
 /* ------------------------------------------------------------ inspection */
 enum {
     OUTLETS_META_PAGE_TABLE = 0,        /* host table [max_slots, max_pages_per_seq], -1 = none */

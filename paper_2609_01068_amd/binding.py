@@ -81,6 +81,19 @@ class outlets_sim_config(C.Structure):
                 ("queue_order", C.c_int32), ("iter_base_us", C.c_int64), ("iter_per_seq_us", C.c_int64)]
 
 
+class outlets_page_state(C.Structure):
+    _fields_ = [("free_bits", C.c_void_p), ("page_table", C.c_void_p), ("seq_len", C.c_void_p),
+                ("num_pages", C.c_int32), ("max_slots", C.c_int32), ("max_seq_len", C.c_int32),
+                ("device", C.c_int32)]
+
+
+class outlets_kv_pages(C.Structure):
+    _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("block_keys", C.c_void_p),
+                ("page_table", C.c_void_p), ("fmt", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("num_pages", C.c_int32), ("max_slots", C.c_int32),
+                ("max_pages", C.c_int32), ("device", C.c_int32)]
+
+
 _lib: Optional[C.CDLL] = None
 
 _P = C.c_void_p
@@ -96,6 +109,18 @@ _SIGS = {
     "outlets_probe_step": (C.c_int, [_P, C.c_int32, _I32P, _P, C.c_int64, _P, _P]),
     "outlets_probe_release": (C.c_int, [_P, C.c_int32, _I32P]),
     "outlets_draft_distribution": (C.c_int, [_P, C.c_int32, _P, _P]),
+    "outlets_pages_reset": (C.c_int, [C.POINTER(outlets_page_state), _P]),
+    "outlets_pages_append": (C.c_int, [C.POINTER(outlets_page_state), C.c_int32, _P, _P, C.c_int32, _P, _P, _P, _P, _P,
+                                       _P, C.c_int64, _P]),
+    "outlets_pages_append_workspace": (C.c_int64, [C.c_int32, C.c_int32]),
+    "outlets_pages_release": (C.c_int, [C.POINTER(outlets_page_state), C.c_int32, _P, _P, _P]),
+    "outlets_cache_write": (C.c_int, [C.POINTER(outlets_kv_pages), C.c_int32, _P, _P, C.c_int64, _P, C.c_int64, _P]),
+    "outlets_block_select": (C.c_int, [C.POINTER(outlets_kv_pages), C.c_int32, _P, _P, _P, C.c_int64, C.c_int32,
+                                       C.c_int32, C.c_int32, C.c_int32, _P, _P, C.c_int64, _P]),
+    "outlets_block_select_workspace": (C.c_int64, [C.POINTER(outlets_kv_pages), C.c_int32]),
+    "outlets_block_attention": (C.c_int, [C.POINTER(outlets_kv_pages), C.c_int32, _P, _P, _P, C.c_int64, C.c_int32, _P,
+                                          C.c_int32, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P]),
+    "outlets_block_attention_workspace": (C.c_int64, [C.POINTER(outlets_kv_pages), C.c_int32, C.c_int32, C.c_int32]),
     "outlets_get_meta": (C.c_int, [_P, C.c_int32, _I32P, C.c_int64, C.POINTER(C.c_int64)]),
     "outlets_get_buffer": (C.c_int, [_P, C.c_int32, _P, C.c_int64, C.POINTER(C.c_int64), _P]),
     "outlets_last_error": (C.c_char_p, []),

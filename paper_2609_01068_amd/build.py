@@ -19,7 +19,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(ROOT, "_build")
 LIB_PATH = os.path.join(PKG, "liboutlets.so")
 
-SOURCES = ["pager.cpp", "sched.cpp", "gemm.hip", "rows.hip", "attn.hip", "api.hip"]
+SOURCES = ["pager.cpp", "sched.cpp", "gemm.hip", "rows.hip", "attn.hip", "pages.hip", "sparse.hip", "api.hip",
+           "paged_api.hip"]
 ARCH = "gfx950"
 
 

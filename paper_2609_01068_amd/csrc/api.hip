@@ -14,6 +14,7 @@
 #include <string>
 #include <vector>
 
+#include "error.hpp"
 #include "kernels.hpp"
 #include "outlets.h"
 #include "pager.hpp"
@@ -25,10 +26,14 @@ namespace {
 
 thread_local std::string g_err;
 
-int fail(int rc, const std::string& msg) {
+}  // namespace
+
+int outlets::fail(int rc, const std::string& msg) {
     g_err = msg;
     return rc;
 }
+
+namespace {
 
 int hip_fail(hipError_t e, const char* what) {
     return fail(OUTLETS_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
