@@ -57,7 +57,7 @@ struct BlockRows {
 };
 int64_t block_select_ws(const KvPages& c, int64_t n_rows);       // bytes
 void launch_block_select(const KvPages& c, const BlockRows& r, int top_k, int sink, int local, int32_t* sel, void* ws,
-                         int64_t ws_bytes, hipStream_t st);
+                         int64_t ws_bytes, int cus, hipStream_t st);
 int64_t block_attention_ws(const KvPages& c, int64_t n_rows, int n_q, int top_k, int cus);    // bytes
 void launch_block_attention(const KvPages& c, const BlockRows& r, const int32_t* sel, int top_k, const void* gate,
                             int64_t ldg, void* out, int64_t ldo, void* ws, int cus, hipStream_t st);

@@ -194,9 +194,10 @@ int outlets_block_select(const outlets_kv_pages* cache, int32_t n_rows, const in
     if (!sel_out) return bad(OUTLETS_ERR_INVALID_ARG, "null sel_out");
     if (cache->max_pages > top_k && (!ws || !aligned16(ws) || ws_bytes < block_select_ws(cache_of(cache), 1)))
         return bad(OUTLETS_ERR_INVALID_ARG, "workspace missing, below one row or not 16-byte aligned");
+    const int cus = compute_units(cache->device);
     return guarded(cache->device, [&] {
         launch_block_select(cache_of(cache), BlockRows{n_rows, row_slot, positions, q, q_stride, n_q_heads}, top_k, sink,
-                            local, sel_out, ws, ws_bytes, static_cast<hipStream_t>(stream));
+                            local, sel_out, ws, ws_bytes, cus, static_cast<hipStream_t>(stream));
     });
 }
 

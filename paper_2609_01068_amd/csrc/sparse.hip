@@ -18,60 +18,203 @@ __device__ __forceinline__ float to_f32(__bf16 x) { return static_cast<float>(x)
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // ---------------------------------------------------------------- scores
-// Order-preserving map of a score to an unsigned key; 0 is below every score.
-// -0 counts as +0 and NaN as -infinity.
-__device__ __forceinline__ uint64_t score_key(double s) {
-    if (s != s) s = -__builtin_inf();
-    s += 0.0;
-    const uint64_t u = __builtin_bit_cast(uint64_t, s);
-    return u ^ ((u >> 63) ? ~0ull : (1ull << 63));
+// Selection is made of comparisons of s_b = max over the group's heads of
+// q_h . kbar_b, and its result is defined by the 64-bit scores.  They are not
+// computed for every page: scores in 32 bits (matrix instructions for bf16)
+// come with a bound on their error, and only pages closer to the border than
+// that bound are scored again in 64 bits.  The first pass is then bound by
+// reading the block keys; at the sizes of a 512-request step (263 candidate
+// pages, 59 wanted) one row in eight scores two or three pages again.
+//
+// Error of a 32-bit score: sums of at most 128 products, each step off by at
+// most 2^-23 of the partial sum's magnitude, hence by 2^-16 sum |q k|; 2^-14
+// leaves a factor of four.  Underflow is covered by the absolute term.
+constexpr float kScoreErr2 = 0x1p-13f;               // twice the bound
+constexpr float kScoreErrAbs = 0x1p-100f;
+
+// What a call selects, and where its scores go.
+struct SelectArgs {
+    KvPages c;
+    const int32_t* row_slot;
+    const int32_t* positions;
+    const void* q;
+    int64_t ldq;
+    int n_rows, G, top_k, sink, local;
+    int tile;              // rows scored together where they belong to one slot
+    uint64_t* keys;        // [rows, n_kv, max_pages]: 64-bit scores of crowded borders
+    float* scores;         // [rows, n_kv, max_pages] (split form)
+    float* bounds;         // [rows, n_kv, chunks] (split form)
+    int32_t* sel;
+};
+
+// Visible pages of row r (0: none).
+__device__ __forceinline__ int visible_pages(const SelectArgs& a, int r) {
+    const int pos = a.positions[r], slot = a.row_slot[r];
+    if (pos < 0 || slot < 0 || slot >= a.c.max_slots) return 0;
+    const int nb = pos / kPage + 1;
+    return nb > a.c.max_pages ? 0 : nb;
 }
 
-// Pages whose scores one workgroup computes.
-constexpr int kScorePages = 128;
+// The rows that the block of row r works on: the whole aligned tile for its
+// first row when the tile's rows share a slot (a prompt's rows: each block
+// key is then read once for all of them), none for the tile's others, and
+// the row alone when they do not.
+__device__ __forceinline__ int block_rows(const SelectArgs& a, int r) {
+    if (a.tile == 1) return 1;
+    const int r0 = r / a.tile * a.tile, r1 = min(r0 + a.tile, a.n_rows);
+    bool same = true;
+    for (int i = r0 + 1; i < r1; ++i) same = same && a.row_slot[i] == a.row_slot[r0];
+    if (!same) return 1;
+    return r == r0 ? r1 - r0 : 0;
+}
 
-// s_b = max over the group's heads of q_h . kbar_b, in 64 bits: a selection
-// is made of comparisons, and with 64-bit sums of exact products scores that
-// differ in the inputs do not tie or swap by the order of a sum.  Four lanes a
-// page and head group.
-template <typename T, int HD>
-__global__ void __launch_bounds__(256)
-block_scores(KvPages c, int row0, const int32_t* __restrict__ row_slot, const int32_t* __restrict__ positions,
-             const T* __restrict__ q, int64_t ldq, int G, int top_k, int sink, int local, int stride,
-             uint64_t* __restrict__ keys) {
-    extern __shared__ double lq[];                   // [G][HD]
-    const int r = row0 + blockIdx.x, g = blockIdx.y, p0 = blockIdx.z * kScorePages;
-    const int pos = positions[r], slot = row_slot[r];
-    if (pos < 0 || slot < 0 || slot >= c.max_slots) return;
-    const int nb = pos / kPage + 1;
-    if (nb > c.max_pages || nb <= top_k) return;
-    const int lo = max(p0, sink), hi = min(p0 + kScorePages, nb - local);
-    if (lo >= hi) return;
-    for (int e = threadIdx.x; e < G * HD; e += 256)
-        lq[e] = to_f64(q[r * ldq + static_cast<int64_t>(g) * G * HD + e]);
-    __syncthreads();
-    constexpr int LP = 16, CH = HD / LP;             // lanes a page, channels a lane
-    const int ln = threadIdx.x % LP;
-    for (int b = p0 + threadIdx.x / LP; b < p0 + kScorePages; b += 256 / LP) {
-        if (b < lo || b >= hi) continue;             // uniform over a page's lanes
-        const int page = c.page_table[static_cast<int64_t>(slot) * c.max_pages + b];
-        double s = -__builtin_inf();
-        if (page >= 0 && page < c.num_pages) {
-            const T* kb = static_cast<const T*>(c.block_keys) + (static_cast<int64_t>(page) * c.n_kv + g) * HD + ln * CH;
-            double kd[CH];
+constexpr int pow2_at_least(int g) { return g <= 1 ? 1 : g <= 2 ? 2 : g <= 4 ? 4 : g <= 8 ? 8 : 16; }
+
+// Scores of pages [p0, p1) for rows r .. r + nr - 1 of one slot and KV head
+// g, by the waves of the block: sc[j * ld + b] of row j and page b (all lo <= b
+// < its last candidate); *bound receives the block's largest sum |q k|.
+//
+// bf16: v_mfma_f32_16x16x32_bf16 with the queries as A (rows: row j's head h
+// at j GP + h, GP the group rounded up to a power of two with the last head
+// repeated) and 16 pages as B; a lane then holds four heads of one page and
+// the group's maximum takes at most two lane exchanges.  The same product of
+// absolute values gives the bound.  A wave takes 64 pages at a time: one
+// coalesced read of their ids, then 16 loads in flight.
+template <int HD, int GP>
+__device__ __forceinline__ void score_pages_bf16(const SelectArgs& a, int r, int nr, int g, int p0, int p1, float* sc,
+                                                 int64_t ld, int nw, uint32_t* bound) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+    const __bf16* q = static_cast<const __bf16*>(a.q);
+    const __bf16* keys = static_cast<const __bf16*>(a.c.block_keys);
+    const int32_t* row = a.c.page_table + static_cast<int64_t>(a.row_slot[r]) * a.c.max_pages;
+    bf16x8 qf[HD / 32], qm[HD / 32];
+    {
+        const int j = min(col / GP, nr - 1), h = min(col % GP, a.G - 1);
+        const __bf16* src = q + (r + j) * a.ldq + (static_cast<int64_t>(g) * a.G + h) * HD + 8 * grp;
+        const bool vec = (reinterpret_cast<uintptr_t>(q) & 15) == 0 && a.ldq % 8 == 0;
 #pragma unroll
-            for (int e = 0; e < CH; ++e) kd[e] = to_f64(kb[e]);
-            for (int h = 0; h < G; ++h) {
-                double a = 0.0;
+        for (int b = 0; b < HD / 32; ++b) {
+            uint4 x;
+            if (vec) {
+                x = *reinterpret_cast<const uint4*>(src + 32 * b);
+            } else {
+                __bf16 e[8];
 #pragma unroll
-                for (int e = 0; e < CH; ++e) a = fma(kd[e], lq[h * HD + ln * CH + e], a);
+                for (int i = 0; i < 8; ++i) e[i] = src[32 * b + i];
+                x = *reinterpret_cast<const uint4*>(e);
+            }
+            qf[b] = __builtin_bit_cast(bf16x8, x);
+            x.x &= 0x7FFF7FFFu; x.y &= 0x7FFF7FFFu; x.z &= 0x7FFF7FFFu; x.w &= 0x7FFF7FFFu;
+            qm[b] = __builtin_bit_cast(bf16x8, x);
+        }
+    }
+    // last candidates of the rows this lane stores
+    constexpr int RL = GP >= 4 ? 1 : 4 / GP;         // rows of a lane's four values
+    int hi[RL];
+    const int j0 = GP >= 4 ? grp / (GP / 4) : grp * RL;
 #pragma unroll
-                for (int o = 1; o < LP; o <<= 1) a += __shfl_xor(a, o, 64);
-                s = a > s ? a : s;                   // NaN: never larger
+    for (int i = 0; i < RL; ++i) {
+        const int nb = j0 + i < nr ? visible_pages(a, r + j0 + i) : 0;
+        hi[i] = nb > a.top_k ? nb - a.local : 0;
+    }
+    uint32_t big = 0;
+    const int tiles = (p1 - p0 + 15) / 16;
+    const int t0 = tiles * w / nw, t1 = tiles * (w + 1) / nw;
+    for (int t = t0; t < t1; t += 4) {
+        const int mine = p0 + 16 * t + lane;
+        int id = mine < p1 && 16 * t + lane < 16 * t1 ? row[mine] : -1;
+        if (id >= a.c.num_pages) id = -1;
+        uint4 kf[4][HD / 32];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t page = max(__shfl(id, 16 * u + col, 64), 0);
+            const __bf16* src = keys + (page * a.c.n_kv + g) * HD + 8 * grp;
+            if (t + u < t1)
+#pragma unroll
+                for (int b = 0; b < HD / 32; ++b) kf[u][b] = *reinterpret_cast<const uint4*>(src + 32 * b);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (t + u >= t1) break;
+            f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f}, m = s;
+#pragma unroll
+            for (int b = 0; b < HD / 32; ++b) {
+                uint4 x = kf[u][b];
+                s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[b], __builtin_bit_cast(bf16x8, x), s, 0, 0, 0);
+                x.x &= 0x7FFF7FFFu; x.y &= 0x7FFF7FFFu; x.z &= 0x7FFF7FFFu; x.w &= 0x7FFF7FFFu;
+                m = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qm[b], __builtin_bit_cast(bf16x8, x), m, 0, 0, 0);
+            }
+            const int b = p0 + 16 * (t + u) + col;
+            const bool there = __shfl(id, 16 * u + col, 64) >= 0;
+            float v[RL];
+#pragma unroll
+            for (int i = 0; i < RL; ++i) {
+                v[i] = s[i * (4 / RL)];
+#pragma unroll
+                for (int e = 1; e < 4 / RL; ++e) v[i] = fmaxf(v[i], s[i * (4 / RL) + e]);
+                if (GP >= 8) v[i] = fmaxf(v[i], __shfl_xor(v[i], 16, 64));
+                if (GP >= 16) v[i] = fmaxf(v[i], __shfl_xor(v[i], 32, 64));
+                if (b >= a.sink && b < hi[i]) {
+                    sc[(j0 + i) * ld + b] = there ? v[i] : -INFINITY;
+                    if (there)
+#pragma unroll
+                        for (int e = 0; e < 4 / RL; ++e)     // as integers: NaN above infinity
+                            big = max(big, __float_as_uint(m[i * (4 / RL) + e]));
+                }
             }
         }
-        if (ln == 0) keys[(static_cast<int64_t>(blockIdx.x) * c.n_kv + g) * stride + b] = score_key(s);
     }
+    if (big) atomicMax(bound, big);
+}
+
+// fp32: 16 lanes a page, on the vector units.
+template <int HD>
+__device__ __forceinline__ void score_pages_f32(const SelectArgs& a, int r, int nr, int g, int p0, int p1, float* sc,
+                                                int64_t ld, int nw, uint32_t* bound) {
+    constexpr int LP = 16, CH = HD / LP;
+    const float* q = static_cast<const float*>(a.q);
+    const float* keys = static_cast<const float*>(a.c.block_keys);
+    const int32_t* row = a.c.page_table + static_cast<int64_t>(a.row_slot[r]) * a.c.max_pages;
+    const int ln = threadIdx.x % LP;
+    uint32_t big = 0;
+    for (int j = 0; j < nr; ++j) {
+        const int nb = visible_pages(a, r + j), hi = nb > a.top_k ? min(nb - a.local, p1) : 0;
+        for (int b = max(p0, a.sink) + static_cast<int>(threadIdx.x) / LP; b < hi; b += nw * 64 / LP) {
+            const int page = row[b];
+            float s = -INFINITY;
+            if (page >= 0 && page < a.c.num_pages) {
+                const float* kb = keys + (static_cast<int64_t>(page) * a.c.n_kv + g) * HD + ln * CH;
+                float kr[CH];
+#pragma unroll
+                for (int e = 0; e < CH; ++e) kr[e] = kb[e];
+                for (int h = 0; h < a.G; ++h) {
+                    const float* qr = q + (r + j) * a.ldq + (static_cast<int64_t>(g) * a.G + h) * HD + ln * CH;
+                    float x = 0.f, m = 0.f;
+#pragma unroll
+                    for (int e = 0; e < CH; ++e) {
+                        x = fmaf(kr[e], qr[e], x);
+                        m = fmaf(fabsf(kr[e]), fabsf(qr[e]), m);
+                    }
+#pragma unroll
+                    for (int o = 1; o < LP; o <<= 1) {
+                        x += __shfl_xor(x, o, 64);
+                        m += __shfl_xor(m, o, 64);
+                    }
+                    s = fmaxf(s, x);
+                    big = max(big, __float_as_uint(m));
+                }
+            }
+            if (ln == 0) sc[j * ld + b] = s;
+        }
+    }
+    if (big) atomicMax(bound, big);
+}
+
+template <typename T, int HD, int GP>
+__device__ __forceinline__ void score_pages(const SelectArgs& a, int r, int nr, int g, int p0, int p1, float* sc,
+                                            int64_t ld, int nw, uint32_t* bound) {
+    if constexpr (sizeof(T) == 2) score_pages_bf16<HD, GP>(a, r, nr, g, p0, p1, sc, ld, nw, bound);
+    else score_pages_f32<HD>(a, r, nr, g, p0, p1, sc, ld, nw, bound);
 }
 
 // ---------------------------------------------------------------- selection
@@ -85,86 +228,356 @@ __device__ __forceinline__ int wave_inclusive(int v) {
     return v;
 }
 
-// One workgroup per row and KV head: the m-th largest key by an eight-bit
-// radix search, then the pages above it and the first ones equal to it, in
-// page order.
-__global__ void __launch_bounds__(256)
-block_pick(KvPages c, int row0, const int32_t* __restrict__ row_slot, const int32_t* __restrict__ positions, int top_k,
-           int sink, int local, int stride, const uint64_t* __restrict__ all_keys, int32_t* __restrict__ sel_out) {
-    const int r = row0 + blockIdx.x, g = blockIdx.y, tid = threadIdx.x;
-    int32_t* sel = sel_out + (static_cast<int64_t>(r) * c.n_kv + g) * top_k;
-    const int pos = positions[r], slot = row_slot[r];
-    int nb = pos < 0 || slot < 0 || slot >= c.max_slots ? 0 : pos / kPage + 1;
-    if (nb > c.max_pages) nb = 0;
-    if (nb <= top_k) {
-        for (int i = tid; i < top_k; i += 256) sel[i] = i < nb ? i : -1;
-        return;
-    }
-    const uint64_t* keys = all_keys + (static_cast<int64_t>(blockIdx.x) * c.n_kv + g) * stride;
-    const int lo = sink, hi = nb - local;
-    int want = top_k - sink - local;                 // at most hi - lo
-    __shared__ int hist[256];
-    __shared__ uint64_t sh_prefix;
-    __shared__ int sh_want;
-    uint64_t prefix = 0;
-    if (want > 0) {
-        for (int shift = 56; shift >= 0; shift -= 8) {
-            hist[tid] = 0;
-            __syncthreads();
-            for (int b = lo + tid; b < hi; b += 256) {
-                const uint64_t key = keys[b];
-                if (shift == 56 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(key >> shift) & 255], 1);
-            }
-            __syncthreads();
-            if (tid < 64) {                          // bins 255 - 4 tid .. 252 - 4 tid, largest first
-                int h[4], sum = 0;
+// Order-preserving maps of scores to unsigned keys; -0 counts as +0 and, in
+// 64 bits, NaN as -infinity.
+__device__ __forceinline__ uint32_t order_key(float s) {
+    const uint32_t u = __float_as_uint(s + 0.f);
+    return u ^ ((u >> 31) ? ~0u : (1u << 31));
+}
+__device__ __forceinline__ uint64_t order_key(double s) {
+    if (s != s) s = -__builtin_inf();
+    const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
+    return u ^ ((u >> 63) ? ~0ull : (1ull << 63));
+}
+
+constexpr int kNear = 256;           // candidates that are compared one with another
+
+template <int NT>
+struct PickShared {
+    int hist[256];
+    int red[NT / 64][2];
+    float fred[NT / 64][2];
+    float value[kNear];
+    int index[kNear];
+    double exact[kNear];
+    uint64_t prefix;
+    int bin, want, count, n;
+    float t;
+};
+
+// Sums of a and b over the block, in every thread.
+template <int NT>
+__device__ __forceinline__ int2 block_sum2(int a, int b, PickShared<NT>& sh) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum += h[j] = hist[255 - 4 * tid - j];
-                int before = wave_inclusive(sum) - sum;
-                if (before < want && before + sum >= want) {
-                    for (int j = 0; j < 4; ++j) {
-                        if (before + h[j] >= want) {
-                            sh_prefix = prefix | (static_cast<uint64_t>(255 - 4 * tid - j) << shift);
-                            sh_want = want - before;
-                            break;
-                        }
-                        before += h[j];
+    for (int o = 32; o > 0; o >>= 1) { a += __shfl_xor(a, o, 64); b += __shfl_xor(b, o, 64); }
+    if ((threadIdx.x & 63) == 0) { sh.red[threadIdx.x >> 6][0] = a; sh.red[threadIdx.x >> 6][1] = b; }
+    __syncthreads();
+    int2 t = make_int2(0, 0);
+    for (int i = 0; i < NT / 64; ++i) { t.x += sh.red[i][0]; t.y += sh.red[i][1]; }
+    __syncthreads();
+    return t;
+}
+
+// The histogram's bin (largest first) that holds the want-th entry: sh.bin,
+// the rank within it in sh.want and its size in sh.count.
+template <int NT>
+__device__ __forceinline__ void find_bin(int want, PickShared<NT>& sh) {
+    if (threadIdx.x < 64) {
+        int h[4], sum = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum += h[j] = sh.hist[255 - 4 * threadIdx.x - j];
+        int before = wave_inclusive(sum) - sum;
+        if (before < want && before + sum >= want) {
+            for (int j = 0; j < 4; ++j) {
+                if (before + h[j] >= want) {
+                    sh.bin = 255 - 4 * threadIdx.x - j;
+                    sh.want = want - before;
+                    sh.count = h[j];
+                    break;
+                }
+                before += h[j];
+            }
+        }
+    }
+    __syncthreads();
+}
+
+// The want-th largest key of those that key(i, k) names for i in [lo, hi), by
+// eight bits at a time; *left receives how many keys equal to it are wanted.
+template <int NT, typename K, typename F>
+__device__ __forceinline__ K radix_select(int lo, int hi, int want, F key, int* left, PickShared<NT>& sh) {
+    K prefix = 0;
+    constexpr int top = 8 * sizeof(K) - 8;
+    for (int shift = top; shift >= 0; shift -= 8) {
+        for (int i = threadIdx.x; i < 256; i += NT) sh.hist[i] = 0;
+        __syncthreads();
+        for (int i = lo + threadIdx.x; i < hi; i += NT) {
+            K k;
+            if (key(i, k) && (shift == top || (k >> (shift + 8)) == (prefix >> (shift + 8))))
+                atomicAdd(&sh.hist[(k >> shift) & 255], 1);
+        }
+        __syncthreads();
+        find_bin<NT>(want, sh);
+        prefix |= static_cast<K>(sh.bin) << shift;
+        want = sh.want;
+        __syncthreads();
+    }
+    *left = want;
+    return prefix;
+}
+
+// 64-bit score of one page, by a wave; every lane gets it.
+template <typename T, int HD>
+__device__ __forceinline__ double exact_score(const KvPages& c, const T* q, int G, int g, int page) {
+    double s = -__builtin_inf();
+    if (page < 0 || page >= c.num_pages) return s;
+    const int lane = threadIdx.x & 63;
+    const T* kb = static_cast<const T*>(c.block_keys) + (static_cast<int64_t>(page) * c.n_kv + g) * HD;
+    for (int h = 0; h < G; ++h) {
+        double a = 0.0;
+#pragma unroll
+        for (int e = 0; e < HD / 64; ++e) a = fma(to_f64(kb[lane + 64 * e]), to_f64(q[h * HD + lane + 64 * e]), a);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) a += __shfl_xor(a, o, 64);
+        s = a > s ? a : s;                           // NaN: never larger
+    }
+    return s;
+}
+
+// The selection of one row and KV head from its scores: pages below `lo`, from
+// `hi` on and the `want` best between them, ascending.  Overwrites scores of
+// the pages that were compared in 64 bits.  All threads of the block.
+template <typename T, int HD, int NT>
+__device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, float bound, uint64_t* keys,
+                         PickShared<NT>& sh) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int lo = a.sink, hi = nb - a.local, want = a.top_k - a.sink - a.local;
+    int32_t* sel = a.sel + (static_cast<int64_t>(r) * a.c.n_kv + g) * a.top_k;
+    const float d2 = bound * kScoreErr2 + kScoreErrAbs;
+    float thr = INFINITY;                            // pages of at least this score are taken
+    if (want > 0) {
+        const bool bounded = d2 < INFINITY;          // not where a product overflows or is NaN
+        float upper = 0.f, lower = 0.f;
+        int need = want, crowd = hi - lo;            // of `crowd` pages near the border, `need` are taken
+        if (bounded) {
+            // the want-th largest score: 256 bins between the extremes (a bin
+            // of a linear scale holds few pages, a bin of the first bits
+            // most), then by comparison within its bin
+            float mn = INFINITY, mx = -INFINITY;
+            for (int i = lo + tid; i < hi; i += NT) {
+                const float s = sc[i];
+                mx = fmaxf(mx, s);
+                if (s > -INFINITY) mn = fminf(mn, s);
+            }
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) {
+                mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+                mn = fminf(mn, __shfl_xor(mn, o, 64));
+            }
+            if (lane == 0) { sh.fred[w][0] = mx; sh.fred[w][1] = mn; }
+            for (int i = tid; i < 256; i += NT) sh.hist[i] = 0;
+            if (tid == 0) sh.n = 0;
+            __syncthreads();
+            for (int i = 0; i < NT / 64; ++i) { mx = fmaxf(mx, sh.fred[i][0]); mn = fminf(mn, sh.fred[i][1]); }
+            const float scale = mx > mn ? 255.f / (mx - mn) : 0.f;
+            auto bin = [&](float s) {                // nondecreasing in s
+                return s > mn ? min(static_cast<int>((s - mn) * scale), 255) : 0;
+            };
+            for (int i = lo + tid; i < hi; i += NT) atomicAdd(&sh.hist[bin(sc[i])], 1);
+            __syncthreads();
+            find_bin<NT>(want, sh);
+            float t;
+            if (sh.count <= kNear) {
+                const int B = sh.bin, rank = sh.want - 1, n = sh.count;
+                for (int i = lo + tid; i < hi; i += NT) {
+                    const float s = sc[i];
+                    if (bin(s) == B) sh.value[atomicAdd(&sh.n, 1)] = s;
+                }
+                __syncthreads();
+                for (int i = tid; i < n; i += NT) {
+                    const float v = sh.value[i];
+                    int above = 0;
+                    for (int j = 0; j < n; ++j) above += sh.value[j] > v || (sh.value[j] == v && j < i);
+                    if (above == rank) sh.t = v;
+                }
+                __syncthreads();
+                t = sh.t;
+            } else {
+                int left;
+                const uint32_t k = radix_select<NT, uint32_t>(
+                    lo, hi, want, [&](int i, uint32_t& k) { k = order_key(sc[i]); return true; }, &left, sh);
+                t = __uint_as_float(k ^ ((k >> 31) ? (1u << 31) : ~0u));
+            }
+            upper = t + d2;
+            lower = t - d2;
+            int in = 0, near = 0;
+            for (int i = lo + tid; i < hi; i += NT) {
+                const float s = sc[i];
+                in += s > upper;
+                near += s >= lower && !(s > upper);
+            }
+            const int2 sum = block_sum2<NT>(in, near, sh);
+            need = want - sum.x;
+            crowd = sum.y;
+        }
+        if (bounded && need == crowd) {
+            thr = lower;
+        } else {
+            // the 64-bit scores of the crowd decide, ties by the page index
+            auto near = [&](int i) { return !bounded || (sc[i] >= lower && !(sc[i] > upper)); };
+            const T* q = static_cast<const T*>(a.q) + r * a.ldq + static_cast<int64_t>(g) * a.G * HD;
+            const int32_t* row = a.c.page_table + static_cast<int64_t>(a.row_slot[r]) * a.c.max_pages;
+            thr = bounded ? fmaxf(upper, -__FLT_MAX__) : 0.f;
+            if (crowd <= kNear) {
+                if (tid == 0) sh.n = 0;
+                __syncthreads();
+                for (int i = lo + tid; i < hi; i += NT)
+                    if (near(i)) sh.index[atomicAdd(&sh.n, 1)] = i;
+                __syncthreads();
+                for (int i = w; i < crowd; i += NT / 64) {
+                    const double s = exact_score<T, HD>(a.c, q, a.G, g, row[sh.index[i]]);
+                    if (lane == 0) sh.exact[i] = s;
+                }
+                __syncthreads();
+                for (int i = tid; i < crowd; i += NT) {
+                    const double s = sh.exact[i];
+                    int above = 0;
+                    for (int j = 0; j < crowd; ++j)
+                        above += sh.exact[j] > s || (sh.exact[j] == s && sh.index[j] < sh.index[i]);
+                    sc[sh.index[i]] = above < need ? INFINITY : -INFINITY;
+                }
+                __syncthreads();
+            } else {
+                for (int i = lo + w; i < hi; i += NT / 64) {
+                    if (!near(i)) continue;
+                    const double s = exact_score<T, HD>(a.c, q, a.G, g, row[i]);
+                    if (lane == 0) keys[i] = order_key(s);
+                }
+                __syncthreads();
+                int left;
+                const uint64_t k = radix_select<NT, uint64_t>(
+                    lo, hi, need, [&](int i, uint64_t& k) { if (!near(i)) return false; k = keys[i]; return true; },
+                    &left, sh);
+                int ties = 0;
+                for (int i0 = lo; i0 < hi; i0 += NT) {
+                    const int i = i0 + tid;
+                    const bool mine = i < hi && near(i);
+                    const uint64_t x = mine ? keys[i] : 0;
+                    const bool tie = mine && x == k;
+                    const uint64_t tb = __ballot(tie);
+                    if (lane == 0) sh.red[w][0] = __popcll(tb);
+                    __syncthreads();
+                    int t0 = ties;
+                    for (int j = 0; j < NT / 64; ++j) {
+                        if (j < w) t0 += sh.red[j][0];
+                        ties += sh.red[j][0];
                     }
+                    if (mine) {
+                        const bool take = x > k || (tie && t0 + __popcll(tb & ((1ull << lane) - 1)) < left);
+                        sc[i] = take ? INFINITY : -INFINITY;
+                    }
+                    __syncthreads();
                 }
             }
-            __syncthreads();
-            prefix = sh_prefix;
-            want = sh_want;                          // how many of the keys equal to the prefix so far
         }
     }
-    __shared__ int red[4][2];
-    int done = 0, ties = 0;                          // pages written, equal keys seen
-    for (int b0 = 0; b0 < nb; b0 += 256) {
+    int done = 0;
+    for (int b0 = 0; b0 < nb; b0 += NT) {
         const int b = b0 + tid;
-        bool take = b < nb && (b < lo || b >= hi), tie = false;
-        if (b >= lo && b < hi && want > 0) {
-            const uint64_t key = keys[b];
-            take = key > prefix;
-            tie = key == prefix;
+        const bool take = b < nb && (b < lo || b >= hi || (want > 0 && sc[b] >= thr));
+        const uint64_t m = __ballot(take);
+        if (lane == 0) sh.red[w][0] = __popcll(m);
+        __syncthreads();
+        int at = done;
+        for (int j = 0; j < NT / 64; ++j) {
+            if (j < w) at += sh.red[j][0];
+            done += sh.red[j][0];
         }
-        const int w = tid >> 6, lane = tid & 63;
-        const uint64_t below = (1ull << lane) - 1;
-        const uint64_t tb = __ballot(tie);
-        if (lane == 0) red[w][0] = __popcll(tb);
-        __syncthreads();
-        int t0 = ties;
-        for (int i = 0; i < w; ++i) t0 += red[i][0];
-        for (int i = 0; i < 4; ++i) ties += red[i][0];
-        if (tie && t0 + __popcll(tb & below) < want) take = true;
-        const uint64_t kb = __ballot(take);
-        if (lane == 0) red[w][1] = __popcll(kb);
-        __syncthreads();
-        int k0 = done;
-        for (int i = 0; i < w; ++i) k0 += red[i][1];
-        for (int i = 0; i < 4; ++i) done += red[i][1];
-        if (take) sel[k0 + __popcll(kb & below)] = b;
+        if (take) sel[at + __popcll(m & ((1ull << lane) - 1))] = b;
         __syncthreads();
     }
+}
+
+// A row that reads every page it sees.
+__device__ __forceinline__ void pick_all(const SelectArgs& a, int r, int g, int nb) {
+    int32_t* sel = a.sel + (static_cast<int64_t>(r) * a.c.n_kv + g) * a.top_k;
+    for (int i = threadIdx.x; i < a.top_k; i += blockDim.x) sel[i] = i < nb ? i : -1;
+}
+
+constexpr int kSelectThreads = 256;
+constexpr int kPickThreads = 1024;
+constexpr int kScorePages = 256;     // pages of a block of the split form
+constexpr int kPickLdsPages = 12288; // scores of a row that are copied to LDS there (48 KB)
+
+// One block per KV head and row (or tile of rows): scores in LDS, then the
+// selection.  KV heads are the fast axis of the grid, so the blocks of one
+// head share an XCD's L2 where there are eight heads, and a prompt's rows
+// find the block keys there.
+template <typename T, int HD, int GP>
+__global__ void __launch_bounds__(kSelectThreads)
+block_select_fused(SelectArgs a) {
+    extern __shared__ float sc[];                    // [tile][max_pages]
+    __shared__ PickShared<kSelectThreads> sh;
+    __shared__ uint32_t bound;
+    const int g = blockIdx.x, r = blockIdx.y;
+    const int nr = block_rows(a, r);
+    if (nr == 0) return;
+    int most = 0;
+    for (int j = 0; j < nr; ++j) most = max(most, visible_pages(a, r + j));
+    if (threadIdx.x == 0) bound = 0;
+    __syncthreads();
+    const int ld = a.c.max_pages;
+    if (most > a.top_k) {
+        score_pages<T, HD, GP>(a, r, nr, g, a.sink, most - a.local, sc, ld, kSelectThreads / 64, &bound);
+        __syncthreads();
+    }
+    for (int j = 0; j < nr; ++j) {
+        const int nb = visible_pages(a, r + j);
+        if (nb <= a.top_k) pick_all(a, r + j, g, nb);
+        else
+            pick_row<T, HD>(a, r + j, g, nb, sc + j * ld, __uint_as_float(bound),
+                            a.keys + (static_cast<int64_t>(r + j) * a.c.n_kv + g) * ld, sh);
+    }
+}
+
+// The split form, for few rows over long caches: scores by chunks of pages,
+// then one block per row and KV head.
+template <typename T, int HD, int GP>
+__global__ void __launch_bounds__(kSelectThreads)
+block_scores(SelectArgs a) {
+    __shared__ uint32_t bound;
+    const int g = blockIdx.x, r = blockIdx.y, p0 = blockIdx.z * kScorePages;
+    const int nr = block_rows(a, r);
+    if (nr == 0) return;
+    int most = 0;
+    for (int j = 0; j < nr; ++j) most = max(most, visible_pages(a, r + j));
+    const int p1 = min(p0 + kScorePages, most - a.local);
+    if (threadIdx.x == 0) bound = 0;
+    __syncthreads();
+    if (most > a.top_k && p0 < p1) {
+        score_pages<T, HD, GP>(a, r, nr, g, p0, p1, a.scores + (static_cast<int64_t>(r) * a.c.n_kv + g) * a.c.max_pages,
+                               static_cast<int64_t>(a.c.n_kv) * a.c.max_pages, kSelectThreads / 64, &bound);
+        __syncthreads();
+    }
+    if (threadIdx.x < nr)
+        a.bounds[(static_cast<int64_t>(r + threadIdx.x) * a.c.n_kv + g) * gridDim.z + blockIdx.z] =
+            __uint_as_float(bound);
+}
+
+template <typename T, int HD, bool LDS>
+__global__ void __launch_bounds__(kPickThreads)
+block_pick(SelectArgs a, int chunks) {
+    extern __shared__ float lds[];                   // [max_pages]
+    __shared__ PickShared<kPickThreads> sh;
+    __shared__ uint32_t bound;
+    const int g = blockIdx.x, r = blockIdx.y, nb = visible_pages(a, r);
+    if (nb <= a.top_k) {
+        pick_all(a, r, g, nb);
+        return;
+    }
+    const int64_t item = static_cast<int64_t>(r) * a.c.n_kv + g;
+    float* sc = a.scores + item * a.c.max_pages;
+    if (threadIdx.x == 0) bound = 0;
+    __syncthreads();
+    if (LDS)
+        for (int i = a.sink + threadIdx.x; i < nb - a.local; i += kPickThreads) lds[i] = sc[i];
+    for (int i = threadIdx.x; i < chunks; i += kPickThreads) {
+        const uint32_t b = __float_as_uint(a.bounds[item * chunks + i]);
+        if (b) atomicMax(&bound, b);
+    }
+    __syncthreads();
+    if constexpr (LDS) pick_row<T, HD>(a, r, g, nb, lds, __uint_as_float(bound), a.keys + item * a.c.max_pages, sh);
+    else pick_row<T, HD>(a, r, g, nb, sc, __uint_as_float(bound), a.keys + item * a.c.max_pages, sh);
 }
 
 // ---------------------------------------------------------------- attention
@@ -411,32 +824,77 @@ block_attend_f32(KvPages c, const int32_t* __restrict__ row_slot, const int32_t*
 
 }  // namespace
 
+static int score_chunks(const KvPages& c) { return (c.max_pages + kScorePages - 1) / kScorePages; }
+
 int64_t block_select_ws(const KvPages& c, int64_t n_rows) {
-    return n_rows * c.n_kv * c.max_pages * static_cast<int64_t>(sizeof(uint64_t));
+    // 64-bit keys, 32-bit scores, bounds
+    const int64_t row = c.n_kv * (static_cast<int64_t>(c.max_pages) * 12 + 4 * score_chunks(c));
+    return n_rows * ((row + 15) / 16 * 16);
 }
 
-void launch_block_select(const KvPages& c, const BlockRows& r, int top_k, int sink, int local, int32_t* sel, void* ws,
-                         int64_t ws_bytes, hipStream_t st) {
-    const int G = r.n_q / c.n_kv;
-    const int64_t row_bytes = block_select_ws(c, 1);
-    const int slab = static_cast<int>(std::min<int64_t>(std::max<int64_t>(ws_bytes / row_bytes, 1), r.n_rows));
-    uint64_t* keys = static_cast<uint64_t*>(ws);
-    for (int r0 = 0; r0 < r.n_rows; r0 += slab) {
-        const int n = std::min(slab, r.n_rows - r0);
-        if (c.max_pages > top_k) {
-            const dim3 grid(n, c.n_kv, (c.max_pages + kScorePages - 1) / kScorePages);
-#define OUTLETS_SCORES(T, HD)                                                                                     \
-    hipLaunchKernelGGL((block_scores<T, HD>), grid, dim3(256), sizeof(double) * G * HD, st, c, r0, r.row_slot,      \
-                       r.positions, static_cast<const T*>(r.q), r.ldq, G, top_k, sink, local, c.max_pages, keys)
-            if (c.fmt == OUTLETS_FMT_F32) {
-                if (c.hd == 128) OUTLETS_SCORES(float, 128); else OUTLETS_SCORES(float, 64);
-            } else {
-                if (c.hd == 128) OUTLETS_SCORES(__bf16, 128); else OUTLETS_SCORES(__bf16, 64);
-            }
-#undef OUTLETS_SCORES
+// LDS of a block's scores in the fused form: three or more blocks of a compute unit.
+constexpr int kFusedBytes = 40 << 10;
+
+void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int sink, int local, int32_t* sel, void* ws,
+                         int64_t ws_bytes, int cus, hipStream_t st) {
+    const int G = rows.n_q / c.n_kv, gp = pow2_at_least(G), chunks = score_chunks(c);
+    const int64_t eb = c.fmt == OUTLETS_FMT_F32 ? 4 : 2, row_bytes = block_select_ws(c, 1);
+    // every row sees all it may read: no scores, no workspace
+    const bool plain = c.max_pages <= top_k;
+    const int slab = static_cast<int>(std::min<int64_t>(plain ? rows.n_rows : ws_bytes / row_bytes,
+                                                        std::min(rows.n_rows, 32768)));     // (the grid's y)
+    // Fused where a row's scores fit the LDS share and either the rows fill
+    // the chip or the caches are short: otherwise few blocks read long caches.
+    const bool fused = plain || (c.max_pages * 4 <= kFusedBytes &&
+                                 (static_cast<int64_t>(rows.n_rows) * c.n_kv >= cus || c.max_pages <= kScorePages));
+    int tile = 16 / gp;
+    if (fused && !plain)
+        while (tile > 1 && tile * c.max_pages * 4 > kFusedBytes) tile /= 2;
+    for (int r0 = 0; r0 < rows.n_rows; r0 += slab) {
+        const int n = std::min(slab, rows.n_rows - r0);
+        const int64_t items = static_cast<int64_t>(n) * c.n_kv;
+        uint64_t* keys = static_cast<uint64_t*>(ws);
+        float* scores = plain ? nullptr : reinterpret_cast<float*>(keys + items * c.max_pages);
+        const SelectArgs a{c,     rows.row_slot + r0, rows.positions + r0,
+                           static_cast<const char*>(rows.q) + eb * rows.ldq * r0,
+                           rows.ldq, n, G, top_k, sink, local, plain ? 1 : tile, keys, scores,
+                           plain ? nullptr : scores + items * c.max_pages, sel + static_cast<int64_t>(r0) * c.n_kv * top_k};
+#define OUTLETS_SELECT(T, HD, GP)                                                                                 \
+    do {                                                                                                          \
+        if (fused) {                                                                                              \
+            hipLaunchKernelGGL((block_select_fused<T, HD, GP>), dim3(c.n_kv, n), dim3(kSelectThreads),              \
+                               plain ? 0 : sizeof(float) * a.tile * c.max_pages, st, a);                            \
+        } else {                                                                                                  \
+            hipLaunchKernelGGL((block_scores<T, HD, GP>), dim3(c.n_kv, n, chunks), dim3(kSelectThreads), 0, st, a);   \
+            OUTLETS_PICK(T, HD);                                                                                  \
+        }                                                                                                         \
+    } while (0)
+#define OUTLETS_PICK(T, HD)                                                                                       \
+    do {                                                                                                          \
+        if (c.max_pages <= kPickLdsPages)                                                                         \
+            hipLaunchKernelGGL((block_pick<T, HD, true>), dim3(c.n_kv, n), dim3(kPickThreads),                      \
+                               sizeof(float) * c.max_pages, st, a, chunks);                                         \
+        else                                                                                                      \
+            hipLaunchKernelGGL((block_pick<T, HD, false>), dim3(c.n_kv, n), dim3(kPickThreads), 0, st, a, chunks);    \
+    } while (0)
+#define OUTLETS_SELECT_G(HD)                                                                                      \
+    switch (gp) {                                                                                                 \
+        case 1: OUTLETS_SELECT(__bf16, HD, 1); break;                                                             \
+        case 2: OUTLETS_SELECT(__bf16, HD, 2); break;                                                             \
+        case 4: OUTLETS_SELECT(__bf16, HD, 4); break;                                                             \
+        case 8: OUTLETS_SELECT(__bf16, HD, 8); break;                                                             \
+        default: OUTLETS_SELECT(__bf16, HD, 16); break;                                                           \
+    }
+        if (c.fmt == OUTLETS_FMT_F32) {
+            if (c.hd == 128) OUTLETS_SELECT(float, 128, 1); else OUTLETS_SELECT(float, 64, 1);
+        } else if (c.hd == 128) {
+            OUTLETS_SELECT_G(128)
+        } else {
+            OUTLETS_SELECT_G(64)
         }
-        hipLaunchKernelGGL(block_pick, dim3(n, c.n_kv), dim3(256), 0, st, c, r0, r.row_slot, r.positions, top_k, sink,
-                           local, c.max_pages, keys, sel);
+#undef OUTLETS_SELECT_G
+#undef OUTLETS_PICK
+#undef OUTLETS_SELECT
     }
 }
 

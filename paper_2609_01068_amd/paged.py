@@ -193,8 +193,11 @@ class PagedKV:
                 out = torch.empty(shape, dtype=torch.int32, device=self.device)
             elif tuple(out.shape) != shape or out.dtype != torch.int32 or not out.is_contiguous() or out.device != self.device:
                 raise TypeError(f"out must be a contiguous int32 tensor of shape {shape} on {self.device}")
-            need = min(B.lib().outlets_block_select_workspace(self._ref, n), _SELECT_WS)
-            need = max(need, B.lib().outlets_block_select_workspace(self._ref, min(n, 1)))
+            need = 0
+            if self.tables.max_pages > top_k and n:
+                need = B.lib().outlets_block_select_workspace(self._ref, n)
+                if need > _SELECT_WS:
+                    need = max(_SELECT_WS, B.lib().outlets_block_select_workspace(self._ref, 1))
             ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
             rc = B.lib().outlets_block_select(self._ref, n, rp, pp, qp, qs, n_q, top_k, sink, local, out.data_ptr(),
                                               ws.data_ptr() if need else None, need, st)

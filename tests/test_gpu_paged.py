@@ -395,6 +395,67 @@ def test_select_in_parts(monkeypatch):
         assert np.array_equal(kv.select(q, i32(rs), i32(pos), 20, 1, 2).cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("fmt", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["ties", "near", "overflow", "nan", "zero", "holes"])
+def test_select_crowded_borders(fmt, kind):
+    """More pages near the border than are compared one with another: equal
+    scores, scores that only 64 bits tell apart, products past the fp32
+    range, NaN, and zero queries."""
+    n_kv, G, hd, top_k = 2, 4, 128, 40
+    table, slots = scattered([16 * 700, 16 * 430 + 3, 16 * 50], 1200, 710, 4)
+    k = randn((1200, n_kv, hd), fmt, 3, 0.3)
+    q = randn((3, n_kv * G, hd), fmt, 4)
+    if kind in ("ties", "near"):
+        k[:] = k[0].clone()
+        if kind == "near":                          # 2^-30 apart, and in no page order
+            k[:, :, 17] = (2.0**-30 * torch.randperm(1200, device="cuda").add(1)[:, None] / 4096).to(k.dtype)
+            q[:, :, 17] = 1.0
+        else:
+            k[torch.as_tensor(table[slots[0], [5, 300, 650]].astype(np.int64), device="cuda")] *= 1.5
+    elif kind == "overflow":
+        k[:, :, 3] = 3e38 * torch.sign(k[:, :, 3])
+        q[:, :, 3] = 8.0
+    elif kind == "nan":
+        k[torch.as_tensor(table[slots[0], 100].astype(np.int64), device="cuda")] = float("nan")
+        q[1, 3, 7] = float("nan")
+        q[2] = float("inf")
+    elif kind == "zero":
+        q[0] = 0
+        k[:, :, 9] = -0.0
+    else:
+        table[slots[0], 20:690] = -1
+        table[slots[1], 2:400:2] = 1200
+    kv = cache_over(table, 1200, n_kv, hd, fmt, block_keys=k)
+    pos = np.array([16 * 700 - 1, 16 * 430 + 2, 16 * 50 - 1], dtype=np.int32)
+    got = kv.select(q, i32(slots), i32(pos), top_k, 2, 3).cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        want = plain_select(k.double().cpu().numpy(), q.double().cpu().numpy(), table, slots, pos, n_kv, top_k, 2, 3)
+    assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("fmt,G", [("f32", 2), ("bf16", 1), ("bf16", 2), ("bf16", 4), ("bf16", 8), ("bf16", 16)])
+@pytest.mark.parametrize("lens", [(4000, 4000), (170000,), (210000, 9000)])
+def test_select_long_and_shared(fmt, G, lens):
+    """Consecutive rows of one request beside rows of another, in tables whose
+    scores fit LDS for several rows, for none while chunks are scored apart,
+    and not at all."""
+    n_kv, hd, top_k = 2, 64, 48
+    num = sum(-(-n // PAGE) for n in lens) + 3
+    table, slots = scattered(lens, num, max(-(-n // PAGE) for n in lens), 4)
+    k = randn((num, n_kv, hd), fmt, 3, 0.3)
+    kv = cache_over(table, num, n_kv, hd, fmt, block_keys=k)
+    row_slot, pos = [], []
+    for s, n in zip(slots, lens):
+        for t in (5, 18):
+            row_slot += [s] * t + [-1]
+            pos += list(range(n - t, n)) + [0]
+    pos[3], pos[6] = 100, lens[0] // 2
+    q = randn((len(pos), n_kv * G, hd), fmt, 4)
+    got = kv.select(q, i32(row_slot), i32(pos), top_k, 1, 2).cpu().numpy()
+    want = plain_select(k.double().cpu().numpy(), q.double().cpu().numpy(), table, row_slot, pos, n_kv, top_k, 1, 2)
+    assert np.array_equal(got, want)
+
+
 # ---------------------------------------------------------------- attention
 
 def attention_ref(kp, vp, q, table, row_slot, pos, sel, gate):
