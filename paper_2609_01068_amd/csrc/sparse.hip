@@ -59,7 +59,7 @@ __device__ __forceinline__ int visible_pages(const SelectArgs& a, int r) {
 // first row when the tile's rows share a slot (a prompt's rows: each block
 // key is then read once for all of them), none for the tile's others, and
 // the row alone when they do not.
-__device__ __forceinline__ int block_rows(const SelectArgs& a, int r) {
+template <typename Args> __device__ __forceinline__ int block_rows(const Args& a, int r) {
     if (a.tile == 1) return 1;
     const int r0 = r / a.tile * a.tile, r1 = min(r0 + a.tile, a.n_rows);
     bool same = true;
@@ -70,9 +70,10 @@ __device__ __forceinline__ int block_rows(const SelectArgs& a, int r) {
 
 constexpr int pow2_at_least(int g) { return g <= 1 ? 1 : g <= 2 ? 2 : g <= 4 ? 4 : g <= 8 ? 8 : 16; }
 
-// Scores of pages [p0, p1) for rows r .. r + nr - 1 of one slot and KV head
-// g, by the waves of the block: sc[j * ld + b] of row j and page b (all lo <= b
-// < its last candidate); *bound receives the block's largest sum |q k|.
+// Scores for rows r .. r + nr - 1 of one slot and KV head g, by one wave:
+// sc[j * ld + b] of row j and page b (where it is a candidate), for `len` pages
+// (at most 64, a multiple of 16) from p0 on, from p0 + step on, .. below p1.
+// Returns the largest sum |q k| that this lane saw, as bits.
 //
 // bf16: v_mfma_f32_16x16x32_bf16 with the queries as A (rows: row j's head h
 // at j GP + h, GP the group rounded up to a power of two with the last head
@@ -81,12 +82,14 @@ constexpr int pow2_at_least(int g) { return g <= 1 ? 1 : g <= 2 ? 2 : g <= 4 ? 4
 // absolute values gives the bound.  A wave takes 64 pages at a time: one
 // coalesced read of their ids, then 16 loads in flight.
 template <int HD, int GP>
-__device__ __forceinline__ void score_pages_bf16(const SelectArgs& a, int r, int nr, int g, int p0, int p1, float* sc,
-                                                 int64_t ld, int nw, uint32_t* bound) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+__device__ __forceinline__ uint32_t score_pages_bf16(const SelectArgs& a, int r, int nr, int g, int p0, int len, int step,
+                                                     int p1, float* sc, int64_t ld) {
+    const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
     const __bf16* q = static_cast<const __bf16*>(a.q);
     const __bf16* keys = static_cast<const __bf16*>(a.c.block_keys);
     const int32_t* row = a.c.page_table + static_cast<int64_t>(a.row_slot[r]) * a.c.max_pages;
+    auto ids = [&](int p) { return lane < len && p + lane < p1 ? row[p + lane] : -1; };
+    int next = ids(p0);
     bf16x8 qf[HD / 32], qm[HD / 32];
     {
         const int j = min(col / GP, nr - 1), h = min(col % GP, a.G - 1);
@@ -118,24 +121,21 @@ __device__ __forceinline__ void score_pages_bf16(const SelectArgs& a, int r, int
         hi[i] = nb > a.top_k ? nb - a.local : 0;
     }
     uint32_t big = 0;
-    const int tiles = (p1 - p0 + 15) / 16;
-    const int t0 = tiles * w / nw, t1 = tiles * (w + 1) / nw;
-    for (int t = t0; t < t1; t += 4) {
-        const int mine = p0 + 16 * t + lane;
-        int id = mine < p1 && 16 * t + lane < 16 * t1 ? row[mine] : -1;
+    for (int p = p0; p < p1; p += step) {
+        int id = next;
+        next = ids(p + step);
         if (id >= a.c.num_pages) id = -1;
         uint4 kf[4][HD / 32];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int64_t page = max(__shfl(id, 16 * u + col, 64), 0);
             const __bf16* src = keys + (page * a.c.n_kv + g) * HD + 8 * grp;
-            if (t + u < t1)
 #pragma unroll
-                for (int b = 0; b < HD / 32; ++b) kf[u][b] = *reinterpret_cast<const uint4*>(src + 32 * b);
+            for (int b = 0; b < HD / 32; ++b) kf[u][b] = *reinterpret_cast<const uint4*>(src + 32 * b);
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            if (t + u >= t1) break;
+            if (16 * u >= len || p + 16 * u >= p1) break;
             f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f}, m = s;
 #pragma unroll
             for (int b = 0; b < HD / 32; ++b) {
@@ -144,7 +144,7 @@ __device__ __forceinline__ void score_pages_bf16(const SelectArgs& a, int r, int
                 x.x &= 0x7FFF7FFFu; x.y &= 0x7FFF7FFFu; x.z &= 0x7FFF7FFFu; x.w &= 0x7FFF7FFFu;
                 m = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qm[b], __builtin_bit_cast(bf16x8, x), m, 0, 0, 0);
             }
-            const int b = p0 + 16 * (t + u) + col;
+            const int b = p + 16 * u + col;
             const bool there = __shfl(id, 16 * u + col, 64) >= 0;
             float v[RL];
 #pragma unroll
@@ -164,13 +164,13 @@ __device__ __forceinline__ void score_pages_bf16(const SelectArgs& a, int r, int
             }
         }
     }
-    if (big) atomicMax(bound, big);
+    return big;
 }
 
 // fp32: 16 lanes a page, on the vector units.
 template <int HD>
-__device__ __forceinline__ void score_pages_f32(const SelectArgs& a, int r, int nr, int g, int p0, int p1, float* sc,
-                                                int64_t ld, int nw, uint32_t* bound) {
+__device__ __forceinline__ uint32_t score_pages_f32(const SelectArgs& a, int r, int nr, int g, int p0, int len, int step,
+                                                    int p1, float* sc, int64_t ld) {
     constexpr int LP = 16, CH = HD / LP;
     const float* q = static_cast<const float*>(a.q);
     const float* keys = static_cast<const float*>(a.c.block_keys);
@@ -179,7 +179,9 @@ __device__ __forceinline__ void score_pages_f32(const SelectArgs& a, int r, int 
     uint32_t big = 0;
     for (int j = 0; j < nr; ++j) {
         const int nb = visible_pages(a, r + j), hi = nb > a.top_k ? min(nb - a.local, p1) : 0;
-        for (int b = max(p0, a.sink) + static_cast<int>(threadIdx.x) / LP; b < hi; b += nw * 64 / LP) {
+        for (int p = p0; p < hi; p += step)
+        for (int b = p + static_cast<int>(threadIdx.x & 63) / LP; b < min(p + len, hi); b += 64 / LP) {
+            if (b < a.sink) continue;                // uniform over a page's lanes
             const int page = row[b];
             float s = -INFINITY;
             if (page >= 0 && page < a.c.num_pages) {
@@ -207,14 +209,14 @@ __device__ __forceinline__ void score_pages_f32(const SelectArgs& a, int r, int 
             if (ln == 0) sc[j * ld + b] = s;
         }
     }
-    if (big) atomicMax(bound, big);
+    return big;
 }
 
 template <typename T, int HD, int GP>
-__device__ __forceinline__ void score_pages(const SelectArgs& a, int r, int nr, int g, int p0, int p1, float* sc,
-                                            int64_t ld, int nw, uint32_t* bound) {
-    if constexpr (sizeof(T) == 2) score_pages_bf16<HD, GP>(a, r, nr, g, p0, p1, sc, ld, nw, bound);
-    else score_pages_f32<HD>(a, r, nr, g, p0, p1, sc, ld, nw, bound);
+__device__ __forceinline__ uint32_t score_pages(const SelectArgs& a, int r, int nr, int g, int p0, int len, int step, int p1,
+                                                float* sc, int64_t ld) {
+    if constexpr (sizeof(T) == 2) return score_pages_bf16<HD, GP>(a, r, nr, g, p0, len, step, p1, sc, ld);
+    else return score_pages_f32<HD>(a, r, nr, g, p0, len, step, p1, sc, ld);
 }
 
 // ---------------------------------------------------------------- selection
@@ -240,10 +242,25 @@ __device__ __forceinline__ uint64_t order_key(double s) {
     return u ^ ((u >> 63) ? ~0ull : (1ull << 63));
 }
 
-constexpr int kNear = 256;           // candidates that are compared one with another
+// Candidates that are compared one with another: a selection by one wave
+// keeps 64, by a block 256.
+constexpr int near_cap(int nt) { return nt == 64 ? 64 : 256; }
+
+// A selection runs on NT threads: a whole block, or one wave, whose LDS
+// accesses are in order and need no barrier.
+template <int NT>
+__device__ __forceinline__ void group_sync() {
+    if constexpr (NT > 64) {
+        __syncthreads();
+    } else {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
 
 template <int NT>
 struct PickShared {
+    static constexpr int kNear = near_cap(NT);
     int hist[256];
     int red[NT / 64][2];
     float fred[NT / 64][2];
@@ -255,16 +272,17 @@ struct PickShared {
     float t;
 };
 
-// Sums of a and b over the block, in every thread.
+// Sums of a and b over the group, in every thread.
 template <int NT>
 __device__ __forceinline__ int2 block_sum2(int a, int b, PickShared<NT>& sh) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) { a += __shfl_xor(a, o, 64); b += __shfl_xor(b, o, 64); }
+    if (NT == 64) return make_int2(a, b);
     if ((threadIdx.x & 63) == 0) { sh.red[threadIdx.x >> 6][0] = a; sh.red[threadIdx.x >> 6][1] = b; }
-    __syncthreads();
+    group_sync<NT>();
     int2 t = make_int2(0, 0);
     for (int i = 0; i < NT / 64; ++i) { t.x += sh.red[i][0]; t.y += sh.red[i][1]; }
-    __syncthreads();
+    group_sync<NT>();
     return t;
 }
 
@@ -272,15 +290,16 @@ __device__ __forceinline__ int2 block_sum2(int a, int b, PickShared<NT>& sh) {
 // the rank within it in sh.want and its size in sh.count.
 template <int NT>
 __device__ __forceinline__ void find_bin(int want, PickShared<NT>& sh) {
-    if (threadIdx.x < 64) {
+    if (NT == 64 || threadIdx.x < 64) {
+        const int lane = threadIdx.x & 63;
         int h[4], sum = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum += h[j] = sh.hist[255 - 4 * threadIdx.x - j];
+        for (int j = 0; j < 4; ++j) sum += h[j] = sh.hist[255 - 4 * lane - j];
         int before = wave_inclusive(sum) - sum;
         if (before < want && before + sum >= want) {
             for (int j = 0; j < 4; ++j) {
                 if (before + h[j] >= want) {
-                    sh.bin = 255 - 4 * threadIdx.x - j;
+                    sh.bin = 255 - 4 * lane - j;
                     sh.want = want - before;
                     sh.count = h[j];
                     break;
@@ -289,46 +308,48 @@ __device__ __forceinline__ void find_bin(int want, PickShared<NT>& sh) {
             }
         }
     }
-    __syncthreads();
+    group_sync<NT>();
 }
 
 // The want-th largest key of those that key(i, k) names for i in [lo, hi), by
 // eight bits at a time; *left receives how many keys equal to it are wanted.
 template <int NT, typename K, typename F>
 __device__ __forceinline__ K radix_select(int lo, int hi, int want, F key, int* left, PickShared<NT>& sh) {
+    const int tid = threadIdx.x % NT;
     K prefix = 0;
     constexpr int top = 8 * sizeof(K) - 8;
     for (int shift = top; shift >= 0; shift -= 8) {
-        for (int i = threadIdx.x; i < 256; i += NT) sh.hist[i] = 0;
-        __syncthreads();
-        for (int i = lo + threadIdx.x; i < hi; i += NT) {
+        for (int i = tid; i < 256; i += NT) sh.hist[i] = 0;
+        group_sync<NT>();
+        for (int i = lo + tid; i < hi; i += NT) {
             K k;
             if (key(i, k) && (shift == top || (k >> (shift + 8)) == (prefix >> (shift + 8))))
                 atomicAdd(&sh.hist[(k >> shift) & 255], 1);
         }
-        __syncthreads();
+        group_sync<NT>();
         find_bin<NT>(want, sh);
         prefix |= static_cast<K>(sh.bin) << shift;
         want = sh.want;
-        __syncthreads();
+        group_sync<NT>();
     }
     *left = want;
     return prefix;
 }
 
-// 64-bit score of one page, by a wave; every lane gets it.
+// 64-bit score of one page by 16 lanes; every one of them gets it.
 template <typename T, int HD>
 __device__ __forceinline__ double exact_score(const KvPages& c, const T* q, int G, int g, int page) {
     double s = -__builtin_inf();
     if (page < 0 || page >= c.num_pages) return s;
-    const int lane = threadIdx.x & 63;
-    const T* kb = static_cast<const T*>(c.block_keys) + (static_cast<int64_t>(page) * c.n_kv + g) * HD;
+    constexpr int CH = HD / 16;
+    const int at = (threadIdx.x & 15) * CH;
+    const T* kb = static_cast<const T*>(c.block_keys) + (static_cast<int64_t>(page) * c.n_kv + g) * HD + at;
     for (int h = 0; h < G; ++h) {
         double a = 0.0;
 #pragma unroll
-        for (int e = 0; e < HD / 64; ++e) a = fma(to_f64(kb[lane + 64 * e]), to_f64(q[h * HD + lane + 64 * e]), a);
+        for (int e = 0; e < CH; ++e) a = fma(to_f64(kb[e]), to_f64(q[h * HD + at + e]), a);
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) a += __shfl_xor(a, o, 64);
+        for (int o = 1; o < 16; o <<= 1) a += __shfl_xor(a, o, 64);
         s = a > s ? a : s;                           // NaN: never larger
     }
     return s;
@@ -336,11 +357,12 @@ __device__ __forceinline__ double exact_score(const KvPages& c, const T* q, int 
 
 // The selection of one row and KV head from its scores: pages below `lo`, from
 // `hi` on and the `want` best between them, ascending.  Overwrites scores of
-// the pages that were compared in 64 bits.  All threads of the block.
+// the pages that were compared in 64 bits.  By the NT threads of a group.
 template <typename T, int HD, int NT>
 __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, float bound, uint64_t* keys,
                          PickShared<NT>& sh) {
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int tid = threadIdx.x % NT, lane = tid & 63, w = tid >> 6;
+    constexpr int kNear = PickShared<NT>::kNear;
     const int lo = a.sink, hi = nb - a.local, want = a.top_k - a.sink - a.local;
     int32_t* sel = a.sel + (static_cast<int64_t>(r) * a.c.n_kv + g) * a.top_k;
     const float d2 = bound * kScoreErr2 + kScoreErrAbs;
@@ -367,14 +389,14 @@ __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, f
             if (lane == 0) { sh.fred[w][0] = mx; sh.fred[w][1] = mn; }
             for (int i = tid; i < 256; i += NT) sh.hist[i] = 0;
             if (tid == 0) sh.n = 0;
-            __syncthreads();
+            group_sync<NT>();
             for (int i = 0; i < NT / 64; ++i) { mx = fmaxf(mx, sh.fred[i][0]); mn = fminf(mn, sh.fred[i][1]); }
             const float scale = mx > mn ? 255.f / (mx - mn) : 0.f;
             auto bin = [&](float s) {                // nondecreasing in s
                 return s > mn ? min(static_cast<int>((s - mn) * scale), 255) : 0;
             };
             for (int i = lo + tid; i < hi; i += NT) atomicAdd(&sh.hist[bin(sc[i])], 1);
-            __syncthreads();
+            group_sync<NT>();
             find_bin<NT>(want, sh);
             float t;
             if (sh.count <= kNear) {
@@ -383,14 +405,14 @@ __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, f
                     const float s = sc[i];
                     if (bin(s) == B) sh.value[atomicAdd(&sh.n, 1)] = s;
                 }
-                __syncthreads();
+                group_sync<NT>();
                 for (int i = tid; i < n; i += NT) {
                     const float v = sh.value[i];
                     int above = 0;
                     for (int j = 0; j < n; ++j) above += sh.value[j] > v || (sh.value[j] == v && j < i);
                     if (above == rank) sh.t = v;
                 }
-                __syncthreads();
+                group_sync<NT>();
                 t = sh.t;
             } else {
                 int left;
@@ -420,15 +442,15 @@ __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, f
             thr = bounded ? fmaxf(upper, -__FLT_MAX__) : 0.f;
             if (crowd <= kNear) {
                 if (tid == 0) sh.n = 0;
-                __syncthreads();
+                group_sync<NT>();
                 for (int i = lo + tid; i < hi; i += NT)
                     if (near(i)) sh.index[atomicAdd(&sh.n, 1)] = i;
-                __syncthreads();
-                for (int i = w; i < crowd; i += NT / 64) {
+                group_sync<NT>();
+                for (int i = tid / 16; i < crowd; i += NT / 16) {
                     const double s = exact_score<T, HD>(a.c, q, a.G, g, row[sh.index[i]]);
-                    if (lane == 0) sh.exact[i] = s;
+                    if (tid % 16 == 0) sh.exact[i] = s;
                 }
-                __syncthreads();
+                group_sync<NT>();
                 for (int i = tid; i < crowd; i += NT) {
                     const double s = sh.exact[i];
                     int above = 0;
@@ -436,14 +458,15 @@ __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, f
                         above += sh.exact[j] > s || (sh.exact[j] == s && sh.index[j] < sh.index[i]);
                     sc[sh.index[i]] = above < need ? INFINITY : -INFINITY;
                 }
-                __syncthreads();
+                group_sync<NT>();
             } else {
-                for (int i = lo + w; i < hi; i += NT / 64) {
+                for (int i = lo + tid / 16; i < hi; i += NT / 16) {
                     if (!near(i)) continue;
                     const double s = exact_score<T, HD>(a.c, q, a.G, g, row[i]);
-                    if (lane == 0) keys[i] = order_key(s);
+                    if (tid % 16 == 0) keys[i] = order_key(s);
                 }
-                __syncthreads();
+                __threadfence_block();
+                group_sync<NT>();
                 int left;
                 const uint64_t k = radix_select<NT, uint64_t>(
                     lo, hi, need, [&](int i, uint64_t& k) { if (!near(i)) return false; k = keys[i]; return true; },
@@ -456,7 +479,7 @@ __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, f
                     const bool tie = mine && x == k;
                     const uint64_t tb = __ballot(tie);
                     if (lane == 0) sh.red[w][0] = __popcll(tb);
-                    __syncthreads();
+                    group_sync<NT>();
                     int t0 = ties;
                     for (int j = 0; j < NT / 64; ++j) {
                         if (j < w) t0 += sh.red[j][0];
@@ -466,118 +489,143 @@ __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, f
                         const bool take = x > k || (tie && t0 + __popcll(tb & ((1ull << lane) - 1)) < left);
                         sc[i] = take ? INFINITY : -INFINITY;
                     }
-                    __syncthreads();
+                    group_sync<NT>();
                 }
             }
         }
     }
-    int done = 0;
-    for (int b0 = 0; b0 < nb; b0 += NT) {
-        const int b = b0 + tid;
-        const bool take = b < nb && (b < lo || b >= hi || (want > 0 && sc[b] >= thr));
-        const uint64_t m = __ballot(take);
-        if (lane == 0) sh.red[w][0] = __popcll(m);
-        __syncthreads();
-        int at = done;
-        for (int j = 0; j < NT / 64; ++j) {
-            if (j < w) at += sh.red[j][0];
-            done += sh.red[j][0];
-        }
-        if (take) sel[at + __popcll(m & ((1ull << lane) - 1))] = b;
-        __syncthreads();
+    // each wave lists a contiguous part, behind those of the waves before it
+    constexpr int NW = NT / 64;
+    const int part = (nb + NT - 1) / NT * 64, b0 = w * part, b1 = min(b0 + part, nb);
+    auto takes = [&](int b) { return b < b1 && (b < lo || b >= hi || (want > 0 && sc[b] >= thr)); };
+    int at = 0;
+    if (NW > 1) {
+        int n = 0;
+        for (int b = b0; b < b1; b += 64) n += __popcll(__ballot(takes(b + lane)));
+        if (lane == 0) sh.red[w][0] = n;
+        group_sync<NT>();
+        for (int j = 0; j < w; ++j) at += sh.red[j][0];
     }
+    for (int b = b0; b < b1; b += 64) {
+        const bool take = takes(b + lane);
+        const uint64_t m = __ballot(take);
+        if (take) sel[at + __popcll(m & ((1ull << lane) - 1))] = b + lane;
+        at += __popcll(m);
+    }
+    group_sync<NT>();
 }
 
 // A row that reads every page it sees.
+template <int NT>
 __device__ __forceinline__ void pick_all(const SelectArgs& a, int r, int g, int nb) {
     int32_t* sel = a.sel + (static_cast<int64_t>(r) * a.c.n_kv + g) * a.top_k;
-    for (int i = threadIdx.x; i < a.top_k; i += blockDim.x) sel[i] = i < nb ? i : -1;
+    for (int i = threadIdx.x % NT; i < a.top_k; i += NT) sel[i] = i < nb ? i : -1;
 }
 
-constexpr int kSelectThreads = 256;
-constexpr int kPickThreads = 1024;
-constexpr int kScorePages = 256;     // pages of a block of the split form
-constexpr int kPickLdsPages = 12288; // scores of a row that are copied to LDS there (48 KB)
+constexpr int kPickLdsPages = 12288; // scores of a row that the split form copies to LDS (48 KB)
+constexpr int kUnit = 64;            // pages that a wave scores at a time
 
-// One block per KV head and row (or tile of rows): scores in LDS, then the
-// selection.  KV heads are the fast axis of the grid, so the blocks of one
-// head share an XCD's L2 where there are eight heads, and a prompt's rows
-// find the block keys there.
-template <typename T, int HD, int GP>
-__global__ void __launch_bounds__(kSelectThreads)
+// A KV head's part of a block key (256 bytes at 128 channels) falls on few of
+// an L2's channels, the same for every page, so an XCD that worked on one
+// head would use a fraction of its L2: the grids below give each XCD every
+// head (416 prompt rows of 1,650 pages, scores alone: 192 us by head, 75 us
+// by row).
+//
+// Fused form: one block of NW waves per KV head and row (or tile of rows),
+// blocks i and i + 8, which share an XCD, taking the heads of one tile.
+// Scores in LDS by all waves, then a wave per row selects.
+template <typename T, int HD, int GP, int NW>
+__global__ void __launch_bounds__(64 * NW)
 block_select_fused(SelectArgs a) {
     extern __shared__ float sc[];                    // [tile][max_pages]
-    __shared__ PickShared<kSelectThreads> sh;
+    __shared__ PickShared<64> sh[NW];
     __shared__ uint32_t bound;
-    const int g = blockIdx.x, r = blockIdx.y;
+    const int w = threadIdx.x >> 6, ld = a.c.max_pages;
+    const int x = blockIdx.x % 8, y = blockIdx.x / 8, g = y % a.c.n_kv;
+    const int r = (y / a.c.n_kv * 8 + x) * a.tile + blockIdx.y;
+    if (r >= a.n_rows) return;
     const int nr = block_rows(a, r);
     if (nr == 0) return;
     int most = 0;
     for (int j = 0; j < nr; ++j) most = max(most, visible_pages(a, r + j));
-    if (threadIdx.x == 0) bound = 0;
-    __syncthreads();
-    const int ld = a.c.max_pages;
-    if (most > a.top_k) {
-        score_pages<T, HD, GP>(a, r, nr, g, a.sink, most - a.local, sc, ld, kSelectThreads / 64, &bound);
-        __syncthreads();
+    if (most > a.top_k) {                            // uniform over the block
+        if (threadIdx.x == 0) bound = 0;
+        group_sync<64 * NW>();
+        // equal shares of 16 pages; a wave's part begins where the last one's ends
+        const int first = a.sink, end = most - a.local, tiles = (end - first + 15) / 16;
+        const uint32_t big = score_pages<T, HD, GP>(a, r, nr, g, first + 16 * (tiles * w / NW), kUnit, kUnit,
+                                                    min(first + 16 * (tiles * (w + 1) / NW), end), sc, ld);
+        if (big) atomicMax(&bound, big);
+        group_sync<64 * NW>();
     }
-    for (int j = 0; j < nr; ++j) {
+    for (int j = w; j < nr; j += NW) {
         const int nb = visible_pages(a, r + j);
-        if (nb <= a.top_k) pick_all(a, r + j, g, nb);
+        if (nb <= a.top_k) pick_all<64>(a, r + j, g, nb);
         else
-            pick_row<T, HD>(a, r + j, g, nb, sc + j * ld, __uint_as_float(bound),
-                            a.keys + (static_cast<int64_t>(r + j) * a.c.n_kv + g) * ld, sh);
+            pick_row<T, HD, 64>(a, r + j, g, nb, sc + j * ld, __uint_as_float(bound),
+                                a.keys + (static_cast<int64_t>(r + j) * a.c.n_kv + g) * ld, sh[w]);
     }
 }
 
-// The split form, for few rows over long caches: scores by chunks of pages,
-// then one block per row and KV head.
+// Split form, for long tables: units of 64 pages dealt to gridDim.x waves (a
+// multiple of 8), so that an XCD scores the same pages for all rows and heads
+// and finds their block keys in its L2; then one block per row and KV head
+// selects: of 1,024 threads where there are fewer blocks than compute units
+// (48 of 3,750 to 8,192 pages: 18 us against 33 us with 256), else of 256
+// (3,328 of 1,650 pages: 35 us against 122 us).
 template <typename T, int HD, int GP>
-__global__ void __launch_bounds__(kSelectThreads)
+__global__ void __launch_bounds__(64)
 block_scores(SelectArgs a) {
-    __shared__ uint32_t bound;
-    const int g = blockIdx.x, r = blockIdx.y, p0 = blockIdx.z * kScorePages;
+    const int g = blockIdx.y, r = blockIdx.z, slices = gridDim.x;
     const int nr = block_rows(a, r);
     if (nr == 0) return;
     int most = 0;
     for (int j = 0; j < nr; ++j) most = max(most, visible_pages(a, r + j));
-    const int p1 = min(p0 + kScorePages, most - a.local);
-    if (threadIdx.x == 0) bound = 0;
-    __syncthreads();
-    if (most > a.top_k && p0 < p1) {
-        score_pages<T, HD, GP>(a, r, nr, g, p0, p1, a.scores + (static_cast<int64_t>(r) * a.c.n_kv + g) * a.c.max_pages,
-                               static_cast<int64_t>(a.c.n_kv) * a.c.max_pages, kSelectThreads / 64, &bound);
-        __syncthreads();
-    }
+    if (most <= a.top_k) return;
+    uint32_t big = score_pages<T, HD, GP>(a, r, nr, g, blockIdx.x * kUnit, kUnit, slices * kUnit, most - a.local,
+                                          a.scores + (static_cast<int64_t>(r) * a.c.n_kv + g) * a.c.max_pages,
+                                          static_cast<int64_t>(a.c.n_kv) * a.c.max_pages);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) big = max(big, __shfl_xor(big, o, 64));
     if (threadIdx.x < nr)
-        a.bounds[(static_cast<int64_t>(r + threadIdx.x) * a.c.n_kv + g) * gridDim.z + blockIdx.z] =
-            __uint_as_float(bound);
+        a.bounds[(static_cast<int64_t>(r + threadIdx.x) * a.c.n_kv + g) * slices + blockIdx.x] = __uint_as_float(big);
 }
 
-template <typename T, int HD, bool LDS>
+template <typename T, int HD, bool LDS, int kPickThreads>
 __global__ void __launch_bounds__(kPickThreads)
-block_pick(SelectArgs a, int chunks) {
+block_pick(SelectArgs a, int slices) {
     extern __shared__ float lds[];                   // [max_pages]
     __shared__ PickShared<kPickThreads> sh;
     __shared__ uint32_t bound;
     const int g = blockIdx.x, r = blockIdx.y, nb = visible_pages(a, r);
     if (nb <= a.top_k) {
-        pick_all(a, r, g, nb);
+        pick_all<kPickThreads>(a, r, g, nb);
         return;
     }
     const int64_t item = static_cast<int64_t>(r) * a.c.n_kv + g;
     float* sc = a.scores + item * a.c.max_pages;
     if (threadIdx.x == 0) bound = 0;
     __syncthreads();
-    if (LDS)
-        for (int i = a.sink + threadIdx.x; i < nb - a.local; i += kPickThreads) lds[i] = sc[i];
-    for (int i = threadIdx.x; i < chunks; i += kPickThreads) {
-        const uint32_t b = __float_as_uint(a.bounds[item * chunks + i]);
+    if (LDS) {
+        // eight loads in flight: other XCDs wrote the scores, each is a trip to memory
+        for (int i0 = threadIdx.x; i0 < nb; i0 += 8 * kPickThreads) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = sc[min(i0 + k * kPickThreads, nb - 1)];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (i0 + k * kPickThreads < nb) lds[i0 + k * kPickThreads] = v[k];
+        }
+    }
+    for (int i = threadIdx.x; i < slices; i += kPickThreads) {
+        const uint32_t b = __float_as_uint(a.bounds[item * slices + i]);
         if (b) atomicMax(&bound, b);
     }
     __syncthreads();
-    if constexpr (LDS) pick_row<T, HD>(a, r, g, nb, lds, __uint_as_float(bound), a.keys + item * a.c.max_pages, sh);
-    else pick_row<T, HD>(a, r, g, nb, sc, __uint_as_float(bound), a.keys + item * a.c.max_pages, sh);
+    if constexpr (LDS)
+        pick_row<T, HD, kPickThreads>(a, r, g, nb, lds, __uint_as_float(bound), a.keys + item * a.c.max_pages, sh);
+    else
+        pick_row<T, HD, kPickThreads>(a, r, g, nb, sc, __uint_as_float(bound), a.keys + item * a.c.max_pages, sh);
 }
 
 // ---------------------------------------------------------------- attention
@@ -586,13 +634,45 @@ constexpr int kMaxGroup = 16;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// Joins the states (m, l, o) that NW waves left in LDS, in wave order, for
-// the G heads of an item; every thread of the block calls it.  A row without
-// keys gives zeros.
-template <typename T, int HD, int NW>
-__device__ __forceinline__ void join_waves(int G, const float* sm, const float* sl, const float* so, const T* gate,
-                                           T* out) {
-    for (int e = threadIdx.x; e < G * HD; e += 64 * NW) {
+constexpr int kAttendWaves = 4;
+
+// What the attention kernels share: the queries' rows, the selection and
+// where the result goes: to `out`, or, where the entries of an item are split
+// over gridDim.z blocks, each block's state to its record in `rec`.
+struct AttendArgs {
+    KvPages c;
+    const int32_t* row_slot;
+    const int32_t* positions;
+    const void* q;
+    int64_t ldq;
+    int n_rows, G, top_k;
+    int tile;              // rows taken together where they belong to one slot
+    const int32_t* sel;
+    float qscale;
+    const void* gate;
+    int64_t ldg;
+    void* out;
+    int64_t ldo;
+    float* rec;            // [rows, n_kv, G, splits, HD + 2]: m, l, o
+                           // (tile = 1)
+};
+
+// Output element e of an item from its running sum L and output O.  A row
+// without keys gives zeros.
+template <typename T, int HD>
+__device__ __forceinline__ void put_output(const AttendArgs& a, int64_t r, int g, int e, float L, float O) {
+    const int64_t col = static_cast<int64_t>(g) * a.G * HD + e;
+    float y = L == 0.f ? 0.f : O / L;
+    if (a.gate) y /= 1.f + fast_exp2(-1.4426950408889634f * to_f32(static_cast<const T*>(a.gate)[r * a.ldg + col]));
+    static_cast<T*>(a.out)[r * a.ldo + col] = static_cast<T>(y);
+}
+
+// Joins the states (m, l, o) that the block's waves left in LDS, in wave order.
+template <typename T, int HD>
+__device__ __forceinline__ void join_waves(const AttendArgs& a, int64_t r, int g, const float* sm, const float* sl,
+                                           const float* so) {
+    constexpr int NW = kAttendWaves;
+    for (int e = threadIdx.x; e < a.G * HD; e += 64 * NW) {
         const int h = e / HD;
         float M = -INFINITY;
 #pragma unroll
@@ -603,51 +683,104 @@ __device__ __forceinline__ void join_waves(int G, const float* sm, const float* 
             if (sl[w * kMaxGroup + h] == 0.f) continue;          // a wave without keys
             const float f = fast_exp2(sm[w * kMaxGroup + h] - M);
             L = fmaf(sl[w * kMaxGroup + h], f, L);
-            O = fmaf(so[w * G * HD + e], f, O);
+            O = fmaf(so[w * a.G * HD + e], f, O);
         }
-        float y = L == 0.f ? 0.f : O / L;
-        if (gate) y /= 1.f + fast_exp2(-1.4426950408889634f * to_f32(gate[e]));
-        out[e] = static_cast<T>(y);
+        if (a.rec) {
+            float* rec = a.rec + (((r * a.c.n_kv + g) * a.G + h) * gridDim.z + blockIdx.z) * (HD + 2);
+            if (e % HD == 0) { rec[0] = M; rec[1] = L; }
+            rec[2 + e % HD] = O;
+        } else {
+            put_output<T, HD>(a, r, g, e, L, O);
+        }
     }
 }
 
-// bf16: one workgroup of NW waves per row and KV head, wave w the entries
-// w, w + NW, .. of the row's list.  Per 16-key page S = K Q^T by
+constexpr int kMaxSplits = 64;
+
+// Joins the records of an item's splits, in order: one block per row and
+// query head, one thread a channel.  Other XCDs wrote the records, so each
+// read is a trip to memory: the weights in one, then eight outputs a trip.
+template <typename T, int HD>
+__global__ void __launch_bounds__(HD) join_splits(AttendArgs a, int splits) {
+    const int64_t r = blockIdx.y;
+    const int h = blockIdx.x, ch = threadIdx.x, lane = ch & 63;
+    const float* rec = a.rec + (r * a.c.n_kv * a.G + h) * splits * (HD + 2);
+    const float* mine = rec + min(lane, splits - 1) * (HD + 2);
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = rec[min(k, splits - 1) * (HD + 2) + 2 + ch];
+    const float m = mine[0], l = lane < splits ? mine[1] : 0.f;
+    const float M = wave_max(l == 0.f ? -INFINITY : m);
+    const float f = l == 0.f ? 0.f : fast_exp2(m - M);
+    float L = 0.f, O = 0.f;
+    for (int i = 0; i < splits; i += 8) {
+        float next[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) next[k] = rec[min(i + 8 + k, splits - 1) * (HD + 2) + 2 + ch];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (i + k >= splits) break;
+            const float w = __shfl(f, i + k, 64);
+            L = fmaf(__shfl(l, i + k, 64), w, L);
+            O = fmaf(v[k], w, O);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = next[k];
+    }
+    put_output<T, HD>(a, r, h / a.G, h % a.G * HD + ch, L, O);
+}
+
+// bf16: one workgroup per row and KV head (and split), whose waves take the
+// entries of the row's list in turn.  Per 16-key page S = K Q^T by
 // v_mfma_f32_16x16x32_bf16 (the G heads in columns of B, the others zero);
 // its output (lane: head l % 16, keys 4 (l / 16) + i) is the B operand of
 // O^T += V^T P^T by v_mfma_f32_16x16x16_bf16, whose A operand is the
 // transposed value page as it is stored, so no element changes lanes.
 // Softmax statistics in fp32; the probabilities enter the second product as
 // bf16 and the row sum adds the same rounded values.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
 template <int HD>
 struct PageFrag {
     uint4 k[HD / 32];
     uint2 v[HD / 16];
 };
 
-template <int HD>
+// One page's operands.  ONCE: the page is not read again soon (rows of
+// different slots): non-temporal loads, 509 rows of 64 pages 353 -> 335 us;
+// where rows share pages they cost (445 rows of 4 slots: 241 -> 270 us).
+template <int HD, bool ONCE>
 __device__ __forceinline__ void load_page(const KvPages& c, int64_t page, int g, int col, int grp, PageFrag<HD>& f) {
     const __bf16* kb = static_cast<const __bf16*>(c.k_pool) + (page * c.n_kv + g) * kPage * HD + col * HD + 8 * grp;
     const __bf16* vb = static_cast<const __bf16*>(c.v_pool) + (page * c.n_kv + g) * HD * kPage + col * kPage + 4 * grp;
+    if constexpr (ONCE) {
 #pragma unroll
-    for (int b = 0; b < HD / 32; ++b) f.k[b] = *reinterpret_cast<const uint4*>(kb + 32 * b);
+        for (int b = 0; b < HD / 32; ++b)
+            f.k[b] = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kb + 32 * b)));
 #pragma unroll
-    for (int b = 0; b < HD / 16; ++b) f.v[b] = *reinterpret_cast<const uint2*>(vb + 16 * kPage * b);
+        for (int b = 0; b < HD / 16; ++b)
+            f.v[b] = __builtin_bit_cast(uint2, __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(vb + 16 * kPage * b)));
+    } else {
+#pragma unroll
+        for (int b = 0; b < HD / 32; ++b) f.k[b] = *reinterpret_cast<const uint4*>(kb + 32 * b);
+#pragma unroll
+        for (int b = 0; b < HD / 16; ++b) f.v[b] = *reinterpret_cast<const uint2*>(vb + 16 * kPage * b);
+    }
 }
 
+// Adds a page to the running softmax of each column: its first `nkeys` keys (by
+// column; 0 or less: none), of a page that holds `vkeys` (wave-uniform).
 template <int HD>
-__device__ __forceinline__ void add_page(int nkeys, int grp, float qscale, const bf16x8* qb, const PageFrag<HD>& f,
-                                         float& m, float& l, f32x4* o) {
+__device__ __forceinline__ void add_page(int nkeys, int vkeys, int grp, float qscale, const bf16x8* qb,
+                                         const PageFrag<HD>& f, float& m, float& l, f32x4* o) {
     f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int b = 0; b < HD / 32; ++b)
         s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f.k[b]), qb[b], s, 0, 0, 0);
-    const bool part = nkeys < kPage;                 // wave-uniform: the page of the newest token
-    if (part) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (4 * grp + i >= nkeys) s[i] = -INFINITY;
-    }
+    for (int i = 0; i < 4; ++i)
+        if (4 * grp + i >= nkeys) s[i] = -INFINITY;
     float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
@@ -675,50 +808,61 @@ __device__ __forceinline__ void add_page(int nkeys, int grp, float qscale, const
     ps += __shfl_xor(ps, 16, 64);
     ps += __shfl_xor(ps, 32, 64);
     l += ps;
+    const bool part = vkeys < kPage;                 // wave-uniform: the page of the newest token
 #pragma unroll
     for (int b = 0; b < HD / 16; ++b) {
         uint2 vv = f.v[b];
         if (part) {                                  // what stands behind the newest token is not read
-            if (4 * grp + 0 >= nkeys) vv.x &= 0xFFFF0000u;
-            if (4 * grp + 1 >= nkeys) vv.x &= 0x0000FFFFu;
-            if (4 * grp + 2 >= nkeys) vv.y &= 0xFFFF0000u;
-            if (4 * grp + 3 >= nkeys) vv.y &= 0x0000FFFFu;
+            if (4 * grp + 0 >= vkeys) vv.x &= 0xFFFF0000u;
+            if (4 * grp + 1 >= vkeys) vv.x &= 0x0000FFFFu;
+            if (4 * grp + 2 >= vkeys) vv.y &= 0xFFFF0000u;
+            if (4 * grp + 3 >= vkeys) vv.y &= 0x0000FFFFu;
         }
         o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, vv), pb, o[b], 0, 0, 0);
     }
 }
 
-template <int HD, int NW>
-__global__ void __launch_bounds__(64 * NW)
-block_attend_bf16(KvPages c, const int32_t* __restrict__ row_slot, const int32_t* __restrict__ positions,
-                  const __bf16* __restrict__ q, int64_t ldq, int G, const int32_t* __restrict__ sel_in, int top_k,
-                  float qscale, const __bf16* __restrict__ gate, int64_t ldg, __bf16* __restrict__ out, int64_t ldo) {
-    extern __shared__ __attribute__((aligned(16))) float so[];        // [NW][G][HD]
-    __shared__ float sm[NW * kMaxGroup], sl[NW * kMaxGroup];
-    const int64_t r = blockIdx.x;
-    const int g = blockIdx.y;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
-    const int pos = positions[r], slot = row_slot[r];
-    const bool live = pos >= 0 && slot >= 0 && slot < c.max_slots && pos / kPage < c.max_pages;
-    const int32_t* sel = sel_in + (r * c.n_kv + g) * top_k;
-    const int32_t* row = c.page_table + static_cast<int64_t>(live ? slot : 0) * c.max_pages;
-    bf16x8 qb[HD / 32];
+// Query column `col` (of row r, head h of the group), or zeros.
+template <int HD>
+__device__ __forceinline__ void load_query(const AttendArgs& a, int64_t r, int g, int h, bool live, int grp, bf16x8* qb) {
+    const __bf16* src = static_cast<const __bf16*>(a.q) + r * a.ldq + (static_cast<int64_t>(g) * a.G + h) * HD + 8 * grp;
 #pragma unroll
     for (int b = 0; b < HD / 32; ++b) {
-        uint4 x = *reinterpret_cast<const uint4*>(q + r * ldq + (static_cast<int64_t>(g) * G + min(col, G - 1)) * HD +
-                                                  32 * b + 8 * grp);
-        if (col >= G) x = make_uint4(0u, 0u, 0u, 0u);
+        uint4 x = *reinterpret_cast<const uint4*>(src + 32 * b);
+        if (!live) x = make_uint4(0u, 0u, 0u, 0u);
         qb[b] = __builtin_bit_cast(bf16x8, x);
     }
+}
+
+// The slot's row of the page table, or null for a row that sees nothing.
+__device__ __forceinline__ const int32_t* table_row(const AttendArgs& a, int64_t r) {
+    const int pos = a.positions[r], slot = a.row_slot[r];
+    const bool live = pos >= 0 && slot >= 0 && slot < a.c.max_slots && pos / kPage < a.c.max_pages;
+    return live ? a.c.page_table + static_cast<int64_t>(slot) * a.c.max_pages : nullptr;
+}
+
+// Attention of one row (and split) by the block.  so: [NW][G][HD].
+template <int HD, bool ONCE>
+__device__ __forceinline__ void attend_row(const AttendArgs& a, int64_t r, int g, float* so, float* sm, float* sl) {
+    constexpr int NW = kAttendWaves;
+    const KvPages& c = a.c;
+    const int G = a.G, top_k = a.top_k;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+    const int first = blockIdx.z * NW + w, turn = gridDim.z * NW;
+    const int pos = a.positions[r];
+    const int32_t* row = table_row(a, r);
+    const int32_t* sel = a.sel + (r * c.n_kv + g) * top_k;
+    bf16x8 qb[HD / 32];
+    load_query<HD>(a, r, g, min(col, G - 1), col < G, grp, qb);
     float m = -INFINITY, l = 0.f;
     f32x4 o[HD / 16];
 #pragma unroll
     for (int b = 0; b < HD / 16; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (live) {
-        for (int e0 = 0; e0 < top_k; e0 += 64 * NW) {
+    if (row) {
+        for (int e0 = 0; e0 < top_k; e0 += 64 * turn) {
             // 64 entries of this wave, one a lane; entries that are no visible
             // page of the row are dropped here
-            const int e = e0 + lane * NW + w;
+            const int e = e0 + lane * turn + first;
             const int idx = e < top_k ? sel[e] : -1;
             int page = -1;
             if (idx >= 0 && idx <= pos / kPage) page = row[idx];
@@ -728,11 +872,12 @@ block_attend_bf16(KvPages c, const int32_t* __restrict__ row_slot, const int32_t
             PageFrag<HD> cur, nxt;
             int at = __builtin_ctzll(todo);
             todo &= todo - 1;
-            load_page<HD>(c, __shfl(page, at, 64), g, col, grp, cur);
+            load_page<HD, ONCE>(c, __shfl(page, at, 64), g, col, grp, cur);
             while (true) {
                 const int nx = todo ? __builtin_ctzll(todo) : at;
-                load_page<HD>(c, __shfl(page, nx, 64), g, col, grp, nxt);
-                add_page<HD>(pos + 1 - __shfl(idx, at, 64) * kPage, grp, qscale, qb, cur, m, l, o);
+                load_page<HD, ONCE>(c, __shfl(page, nx, 64), g, col, grp, nxt);
+                const int nkeys = pos + 1 - __shfl(idx, at, 64) * kPage;
+                add_page<HD>(nkeys, nkeys, grp, a.qscale, qb, cur, m, l, o);
                 if (!todo) break;
                 todo &= todo - 1;
                 at = nx;
@@ -747,26 +892,158 @@ block_attend_bf16(KvPages c, const int32_t* __restrict__ row_slot, const int32_t
             *reinterpret_cast<f32x4*>(so + (w * G + col) * HD + 16 * b + 4 * grp) = o[b];
     }
     __syncthreads();
-    join_waves<__bf16, HD, NW>(G, sm, sl, so, gate ? gate + r * ldg + static_cast<int64_t>(g) * G * HD : nullptr,
-                               out + r * ldo + static_cast<int64_t>(g) * G * HD);
+    join_waves<__bf16, HD>(a, r, g, sm, sl, so);
+}
+
+// Attention of nr rows of one slot at once: the G heads of each in the columns
+// of one MFMA, over the pages that any of the rows selects, read once.  A page
+// weighs nothing in the columns of rows that do not select it.  Returns false,
+// with nothing that counts written, where that is not the same as row by row:
+// a list that names a page twice, or an output that is not finite (a value of a
+// page that only other rows select may be infinite or NaN, and 0 times it is
+// not 0).  LDS: `buf` holds the pages' row masks and their list, then the states.
+template <int HD>
+__device__ __forceinline__ bool attend_tile(const AttendArgs& a, int64_t r, int nr, int g, float* buf, float* sm,
+                                            float* sl) {
+    constexpr int NW = kAttendWaves;
+    __shared__ int n_list, odd;
+    const KvPages& c = a.c;
+    const int G = a.G, tid = threadIdx.x;
+    const int lane = tid & 63, w = tid >> 6, col = lane & 15, grp = lane >> 4;
+    const int words = (c.max_pages + 1) / 2;
+    uint32_t* mask = reinterpret_cast<uint32_t*>(buf);               // 16 bits a page: rows that select it
+    int32_t* list = reinterpret_cast<int32_t*>(buf) + words;
+    for (int i = tid; i < words; i += 64 * NW) mask[i] = 0;
+    if (tid == 0) n_list = odd = 0;
+    __syncthreads();
+    bool twice = false;
+    int last = -1;                                                   // newest position of the tile
+    const int32_t* row = nullptr;
+    for (int j = 0; j < nr; ++j) {
+        const int32_t* tr = table_row(a, r + j);
+        if (!tr) continue;
+        row = tr;
+        const int pos = a.positions[r + j];
+        last = max(last, pos);
+        const int32_t* sel = a.sel + ((r + j) * c.n_kv + g) * a.top_k;
+        for (int e = tid; e < a.top_k; e += 64 * NW) {
+            const int idx = sel[e];
+            if (idx < 0 || idx > pos / kPage) continue;
+            const uint32_t bit = 1u << (16 * (idx & 1) + j);
+            const uint32_t was = atomicOr(&mask[idx >> 1], bit);
+            twice = twice || (was & bit);
+            if (!(was >> (16 * (idx & 1)) & 0xFFFFu)) list[atomicAdd(&n_list, 1)] = idx;
+        }
+    }
+    if (__syncthreads_or(twice)) return false;
+    const int n = n_list;
+    const int j = min(col / G, nr - 1), h = col % G;
+    const bool mine = col < nr * G;
+    const int pos = mine && table_row(a, r + j) ? a.positions[r + j] : -1;
+    bf16x8 qb[HD / 32];
+    load_query<HD>(a, r + j, g, h, mine, grp, qb);
+    float m = -INFINITY, l = 0.f;
+    f32x4 o[HD / 16];
+#pragma unroll
+    for (int b = 0; b < HD / 16; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int e0 = 0; e0 < n; e0 += 64 * NW) {
+        const int e = e0 + lane * NW + w;
+        const int idx = e < n ? list[e] : -1;
+        int page = idx >= 0 ? row[idx] : -1;
+        if (page >= c.num_pages) page = -1;
+        uint64_t todo = __ballot(page >= 0);
+        if (!todo) continue;
+        PageFrag<HD> cur, nxt;
+        int at = __builtin_ctzll(todo);
+        todo &= todo - 1;
+        load_page<HD, false>(c, __shfl(page, at, 64), g, col, grp, cur);
+        while (true) {
+            const int nx = todo ? __builtin_ctzll(todo) : at;
+            load_page<HD, false>(c, __shfl(page, nx, 64), g, col, grp, nxt);
+            const int b = __shfl(idx, at, 64);
+            const bool takes = mask[b >> 1] >> (16 * (b & 1) + j) & 1u;
+            add_page<HD>(takes ? pos + 1 - b * kPage : 0, last + 1 - b * kPage, grp, a.qscale, qb, cur, m, l, o);
+            if (!todo) break;
+            todo &= todo - 1;
+            at = nx;
+            cur = nxt;
+        }
+    }
+    __syncthreads();                                                 // the masks and the list are done with
+    if (mine) {
+        if (grp == 0) { sm[w * kMaxGroup + col] = m; sl[w * kMaxGroup + col] = l; }
+#pragma unroll
+        for (int b = 0; b < HD / 16; ++b)
+            *reinterpret_cast<f32x4*>(buf + (w * nr * G + col) * HD + 16 * b + 4 * grp) = o[b];
+    }
+    __syncthreads();
+    bool finite = true;
+    for (int e = tid; e < nr * G * HD; e += 64 * NW) {
+        const int x = e / HD;
+        float M = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < NW; ++v) M = fmaxf(M, sm[v * kMaxGroup + x]);
+        float L = 0.f, O = 0.f;
+#pragma unroll
+        for (int v = 0; v < NW; ++v) {
+            // a wave none of whose pages the column selects still carries 0 V in o
+            const float f = sl[v * kMaxGroup + x] == 0.f ? 0.f : fast_exp2(sm[v * kMaxGroup + x] - M);
+            L = fmaf(sl[v * kMaxGroup + x], f, L);
+            O = fmaf(buf[v * nr * G * HD + e], f, O);
+        }
+        finite = finite && fabsf(O) < INFINITY && fabsf(L) < INFINITY;
+        put_output<__bf16, HD>(a, r + x / G, g, x % G * HD + e % HD, L, O);
+    }
+    return !__syncthreads_or(!finite);
+}
+
+// One block per KV head and row (or tile of rows of one slot, where `tile` is
+// not 1).  KV heads are the fast axis of the grid: with eight of them, an XCD
+// works on one and finds pages that rows share in its L2.
+template <int HD, bool ONCE>
+__global__ void __launch_bounds__(64 * kAttendWaves)
+block_attend_bf16(AttendArgs a) {
+    extern __shared__ __attribute__((aligned(16))) float buf[];
+    __shared__ float sm[kAttendWaves * kMaxGroup], sl[kAttendWaves * kMaxGroup];
+    // the tiles' first rows first: blocks with work that stand apart in the
+    // grid, between empty ones, meet on a quarter of the compute units
+    // (445 rows of 4 slots: 404 us, in this order 134 us)
+    const int tiles = gridDim.y / a.tile;
+    const int r = blockIdx.y % tiles * a.tile + blockIdx.y / tiles, g = blockIdx.x;
+    if (r >= a.n_rows) return;
+    const int nr = block_rows(a, r);
+    if (nr == 0) return;
+    if (nr > 1) {
+        if (attend_tile<HD>(a, r, nr, g, buf, sm, sl)) return;
+        for (int j = 0; j < nr; ++j) {
+            attend_row<HD, false>(a, r + j, g, buf, sm, sl);
+            __syncthreads();
+        }
+    } else {
+        attend_row<HD, ONCE>(a, r, g, buf, sm, sl);
+    }
 }
 
 // fp32: the same split, on the vector units.  Scores with 4 lanes a key,
 // outputs with one lane a channel; the heads one after another.
-template <int HD, int NW>
-__global__ void __launch_bounds__(64 * NW)
-block_attend_f32(KvPages c, const int32_t* __restrict__ row_slot, const int32_t* __restrict__ positions,
-                 const float* __restrict__ q, int64_t ldq, int G, const int32_t* __restrict__ sel_in, int top_k,
-                 float qscale, const float* __restrict__ gate, int64_t ldg, float* __restrict__ out, int64_t ldo) {
+template <int HD>
+__global__ void __launch_bounds__(64 * kAttendWaves)
+block_attend_f32(AttendArgs a) {
+    constexpr int NW = kAttendWaves;
     extern __shared__ __attribute__((aligned(16))) float so[];        // [NW][G][HD], then q [G][HD]
     __shared__ float sm[NW * kMaxGroup], sl[NW * kMaxGroup];
+    const KvPages& c = a.c;
+    const float* q = static_cast<const float*>(a.q);
+    const int64_t ldq = a.ldq;
+    const int G = a.G, top_k = a.top_k;
+    const float qscale = a.qscale;
     float* lq = so + NW * G * HD;
-    const int64_t r = blockIdx.x;
-    const int g = blockIdx.y;
+    const int64_t r = blockIdx.y;
+    const int g = blockIdx.x;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int pos = positions[r], slot = row_slot[r];
+    const int pos = a.positions[r], slot = a.row_slot[r];
     const bool live = pos >= 0 && slot >= 0 && slot < c.max_slots && pos / kPage < c.max_pages;
-    const int32_t* sel = sel_in + (r * c.n_kv + g) * top_k;
+    const int32_t* sel = a.sel + (r * c.n_kv + g) * top_k;
     const int32_t* row = c.page_table + static_cast<int64_t>(live ? slot : 0) * c.max_pages;
     for (int e = threadIdx.x; e < G * HD; e += 64 * NW) lq[e] = q[r * ldq + static_cast<int64_t>(g) * G * HD + e];
     for (int e = threadIdx.x; e < NW * G * HD; e += 64 * NW) so[e] = 0.f;
@@ -775,7 +1052,7 @@ block_attend_f32(KvPages c, const int32_t* __restrict__ row_slot, const int32_t*
     constexpr int CK = HD / 4, CV = HD / 64;
     const int key = lane >> 2, part = lane & 3;
     if (live) {
-        for (int e = w; e < top_k; e += NW) {
+        for (int e = blockIdx.z * NW + w; e < top_k; e += gridDim.z * NW) {
             const int idx = sel[e];
             if (idx < 0 || idx > pos / kPage) continue;
             const int page = row[idx];
@@ -809,46 +1086,48 @@ block_attend_f32(KvPages c, const int32_t* __restrict__ row_slot, const int32_t*
 #pragma unroll
                 for (int j = 0; j < CV; ++j) {
                     float* dst = so + (w * G + h) * HD + lane + 64 * j;
-                    float a = *dst * corr;
+                    float y = *dst * corr;
 #pragma unroll
-                    for (int i = 0; i < kPage; ++i) a = fmaf(__shfl(p, 4 * i, 64), vr[j][i], a);
-                    *dst = a;
+                    for (int i = 0; i < kPage; ++i) y = fmaf(__shfl(p, 4 * i, 64), vr[j][i], y);
+                    *dst = y;
                 }
             }
         }
     }
     __syncthreads();
-    join_waves<float, HD, NW>(G, sm, sl, so, gate ? gate + r * ldg + static_cast<int64_t>(g) * G * HD : nullptr,
-                              out + r * ldo + static_cast<int64_t>(g) * G * HD);
+    join_waves<float, HD>(a, r, g, sm, sl, so);
 }
 
 }  // namespace
 
-static int score_chunks(const KvPages& c) { return (c.max_pages + kScorePages - 1) / kScorePages; }
+// Waves that share a row's units in the split form: about three units each
+// where the table is that long.
+static int score_slices(const KvPages& c) { return 8 * std::max(1, (c.max_pages + kUnit - 1) / kUnit / 24); }
 
 int64_t block_select_ws(const KvPages& c, int64_t n_rows) {
     // 64-bit keys, 32-bit scores, bounds
-    const int64_t row = c.n_kv * (static_cast<int64_t>(c.max_pages) * 12 + 4 * score_chunks(c));
+    const int64_t row = c.n_kv * (static_cast<int64_t>(c.max_pages) * 12 + 4 * score_slices(c));
     return n_rows * ((row + 15) / 16 * 16);
 }
 
-// LDS of a block's scores in the fused form: three or more blocks of a compute unit.
-constexpr int kFusedBytes = 40 << 10;
+// Tables up to this many pages take the fused form.
+constexpr int kFusedPages = 1024;
+constexpr int kFusedBytes = 16 << 10;    // LDS of a block's scores there
 
 void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int sink, int local, int32_t* sel, void* ws,
                          int64_t ws_bytes, int cus, hipStream_t st) {
-    const int G = rows.n_q / c.n_kv, gp = pow2_at_least(G), chunks = score_chunks(c);
+    const int G = rows.n_q / c.n_kv, gp = pow2_at_least(G), slices = score_slices(c);
     const int64_t eb = c.fmt == OUTLETS_FMT_F32 ? 4 : 2, row_bytes = block_select_ws(c, 1);
     // every row sees all it may read: no scores, no workspace
     const bool plain = c.max_pages <= top_k;
+    const bool fused = plain || c.max_pages <= kFusedPages;
     const int slab = static_cast<int>(std::min<int64_t>(plain ? rows.n_rows : ws_bytes / row_bytes,
-                                                        std::min(rows.n_rows, 32768)));     // (the grid's y)
-    // Fused where a row's scores fit the LDS share and either the rows fill
-    // the chip or the caches are short: otherwise few blocks read long caches.
-    const bool fused = plain || (c.max_pages * 4 <= kFusedBytes &&
-                                 (static_cast<int64_t>(rows.n_rows) * c.n_kv >= cus || c.max_pages <= kScorePages));
-    int tile = 16 / gp;
-    if (fused && !plain)
+                                                        std::min(rows.n_rows, 32768)));     // (the grid's z)
+    // Enough rows to fill the chip with a wave each, and not so many that slots
+    // must have several of them: one wave per block, none of which waits.
+    const bool alone = fused && rows.n_rows < 2 * c.max_slots && static_cast<int64_t>(rows.n_rows) * c.n_kv >= 8 * cus;
+    int tile = plain || alone ? 1 : 16 / gp;
+    if (fused)
         while (tile > 1 && tile * c.max_pages * 4 > kFusedBytes) tile /= 2;
     for (int r0 = 0; r0 < rows.n_rows; r0 += slab) {
         const int n = std::min(slab, rows.n_rows - r0);
@@ -857,25 +1136,29 @@ void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int
         float* scores = plain ? nullptr : reinterpret_cast<float*>(keys + items * c.max_pages);
         const SelectArgs a{c,     rows.row_slot + r0, rows.positions + r0,
                            static_cast<const char*>(rows.q) + eb * rows.ldq * r0,
-                           rows.ldq, n, G, top_k, sink, local, plain ? 1 : tile, keys, scores,
+                           rows.ldq, n, G, top_k, sink, local, tile, keys, scores,
                            plain ? nullptr : scores + items * c.max_pages, sel + static_cast<int64_t>(r0) * c.n_kv * top_k};
 #define OUTLETS_SELECT(T, HD, GP)                                                                                 \
     do {                                                                                                          \
-        if (fused) {                                                                                              \
-            hipLaunchKernelGGL((block_select_fused<T, HD, GP>), dim3(c.n_kv, n), dim3(kSelectThreads),              \
-                               plain ? 0 : sizeof(float) * a.tile * c.max_pages, st, a);                            \
+        const dim3 blocks((n + 8 * tile - 1) / (8 * tile) * 8 * c.n_kv, tile);                                    \
+        const size_t lds = plain ? 0 : sizeof(float) * tile * c.max_pages;                                        \
+        if (alone) {                                                                                              \
+            hipLaunchKernelGGL((block_select_fused<T, HD, GP, 1>), blocks, dim3(64), lds, st, a);                   \
+        } else if (fused) {                                                                                       \
+            hipLaunchKernelGGL((block_select_fused<T, HD, GP, 4>), blocks, dim3(256), lds, st, a);                  \
         } else {                                                                                                  \
-            hipLaunchKernelGGL((block_scores<T, HD, GP>), dim3(c.n_kv, n, chunks), dim3(kSelectThreads), 0, st, a);   \
-            OUTLETS_PICK(T, HD);                                                                                  \
+            hipLaunchKernelGGL((block_scores<T, HD, GP>), dim3(slices, c.n_kv, n), dim3(64), 0, st, a); \
+            if (items < cus) OUTLETS_PICK(T, HD, 1024);                                                            \
+            else OUTLETS_PICK(T, HD, 256);                                                                         \
         }                                                                                                         \
     } while (0)
-#define OUTLETS_PICK(T, HD)                                                                                       \
+#define OUTLETS_PICK(T, HD, NT)                                                                                   \
     do {                                                                                                          \
         if (c.max_pages <= kPickLdsPages)                                                                         \
-            hipLaunchKernelGGL((block_pick<T, HD, true>), dim3(c.n_kv, n), dim3(kPickThreads),                      \
-                               sizeof(float) * c.max_pages, st, a, chunks);                                         \
+            hipLaunchKernelGGL((block_pick<T, HD, true, NT>), dim3(c.n_kv, n), dim3(NT), sizeof(float) * c.max_pages, st, \
+                               a, slices);                                                                        \
         else                                                                                                      \
-            hipLaunchKernelGGL((block_pick<T, HD, false>), dim3(c.n_kv, n), dim3(kPickThreads), 0, st, a, chunks);    \
+            hipLaunchKernelGGL((block_pick<T, HD, false, NT>), dim3(c.n_kv, n), dim3(NT), 0, st, a, slices);          \
     } while (0)
 #define OUTLETS_SELECT_G(HD)                                                                                      \
     switch (gp) {                                                                                                 \
@@ -898,26 +1181,62 @@ void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int
     }
 }
 
-int64_t block_attention_ws(const KvPages& c, int64_t n_rows, int n_q, int top_k, int cus) { return 0; }
+// Blocks over which an item's entries are split: where there are fewer items
+// than two blocks a compute unit, and as long as a wave has eight pages (six
+// rows of 128 pages, 8 KV heads: 28 us on one block each, 17 us split and joined).
+static int attend_splits(int64_t items, int top_k, int cus) {
+    const int64_t fill = (2 * cus + items - 1) / std::max<int64_t>(items, 1);
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({fill, top_k / (8 * kAttendWaves), kMaxSplits})));
+}
 
-void launch_block_attention(const KvPages& c, const BlockRows& r, const int32_t* sel, int top_k, const void* gate,
+int64_t block_attention_ws(const KvPages& c, int64_t n_rows, int n_q, int top_k, int cus) {
+    const int splits = attend_splits(n_rows * c.n_kv, top_k, cus);
+    return splits == 1 ? 0 : n_rows * n_q * splits * (c.hd + 2) * static_cast<int64_t>(sizeof(float));
+}
+
+// Rows of one launch (the grid's y).
+constexpr int kAttendRows = 32768;
+constexpr int kTileBytes = 32 << 10;     // LDS of a tile's page masks and list
+
+void launch_block_attention(const KvPages& c, const BlockRows& rows, const int32_t* sel, int top_k, const void* gate,
                             int64_t ldg, void* out, int64_t ldo, void* ws, int cus, hipStream_t st) {
-    const int G = r.n_q / c.n_kv;
-    const float qscale = 1.4426950408889634f / sqrtf(static_cast<float>(c.hd));
-    constexpr int NW = 4;
-    const dim3 grid(r.n_rows, c.n_kv), block(64 * NW);
-#define OUTLETS_ATTEND(K, T, HD, LDS)                                                                            \
-    hipLaunchKernelGGL((K<HD, NW>), grid, block, sizeof(float) * G * HD * (LDS), st, c, r.row_slot, r.positions,   \
-                       static_cast<const T*>(r.q), r.ldq, G, sel, top_k, qscale, static_cast<const T*>(gate), ldg,  \
-                       static_cast<T*>(out), ldo)
-    if (c.fmt == OUTLETS_FMT_F32) {
-        if (c.hd == 128) OUTLETS_ATTEND(block_attend_f32, float, 128, NW + 1);
-        else OUTLETS_ATTEND(block_attend_f32, float, 64, NW + 1);
-    } else {
-        if (c.hd == 128) OUTLETS_ATTEND(block_attend_bf16, __bf16, 128, NW);
-        else OUTLETS_ATTEND(block_attend_bf16, __bf16, 64, NW);
-    }
+    const int G = rows.n_q / c.n_kv;
+    const int splits = attend_splits(static_cast<int64_t>(rows.n_rows) * c.n_kv, top_k, cus);
+    const int64_t eb = c.fmt == OUTLETS_FMT_F32 ? 4 : 2;
+    // rows taken together: as many as fill the 16 columns and whose page list
+    // and masks fit the LDS that their states need
+    int tile = c.fmt == OUTLETS_FMT_F32 || splits > 1 ? 1 : 16 / G;
+    while (tile > 1 && 4 * ((c.max_pages + 1) / 2 + static_cast<int64_t>(tile) * top_k) > kTileBytes) tile /= 2;
+    for (int r0 = 0; r0 < rows.n_rows; r0 += kAttendRows) {
+        const int n = std::min(kAttendRows, rows.n_rows - r0);
+        const AttendArgs a{c, rows.row_slot + r0, rows.positions + r0, static_cast<const char*>(rows.q) + eb * rows.ldq * r0,
+                           rows.ldq, n, G, top_k, tile, sel + static_cast<int64_t>(r0) * c.n_kv * top_k,
+                           1.4426950408889634f / sqrtf(static_cast<float>(c.hd)),
+                           gate ? static_cast<const char*>(gate) + eb * ldg * r0 : nullptr, ldg,
+                           static_cast<char*>(out) + eb * ldo * r0, ldo, splits == 1 ? nullptr : static_cast<float*>(ws)};
+        const dim3 grid(c.n_kv, (n + tile - 1) / tile * tile, splits);
+#define OUTLETS_ATTEND(K, T, HD, LDS)                                                                             \
+    do {                                                                                                          \
+        hipLaunchKernelGGL(K, grid, dim3(64 * kAttendWaves), LDS, st, a);                                         \
+        if (splits > 1) hipLaunchKernelGGL((join_splits<T, HD>), dim3(rows.n_q, n), dim3(HD), 0, st, a, splits);     \
+    } while (0)
+        if (c.fmt == OUTLETS_FMT_F32) {
+            const size_t lds = sizeof(float) * G * c.hd * (kAttendWaves + 1);
+            if (c.hd == 128) OUTLETS_ATTEND(block_attend_f32<128>, float, 128, lds);
+            else OUTLETS_ATTEND(block_attend_f32<64>, float, 64, lds);
+        } else {
+            const size_t lds = std::max<size_t>(sizeof(float) * tile * G * c.hd * kAttendWaves,
+                                                tile > 1 ? 4 * ((c.max_pages + 1) / 2 + tile * top_k) : 0);
+            if (splits > 1) {
+                if (c.hd == 128) OUTLETS_ATTEND((block_attend_bf16<128, false>), __bf16, 128, lds);
+                else OUTLETS_ATTEND((block_attend_bf16<64, false>), __bf16, 64, lds);
+            } else {
+                if (c.hd == 128) OUTLETS_ATTEND((block_attend_bf16<128, true>), __bf16, 128, lds);
+                else OUTLETS_ATTEND((block_attend_bf16<64, true>), __bf16, 64, lds);
+            }
+        }
 #undef OUTLETS_ATTEND
+    }
 }
 
 }  // namespace outlets

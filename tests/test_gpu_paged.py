@@ -465,7 +465,7 @@ def attention_ref(kp, vp, q, table, row_slot, pos, sel, gate):
     G = n_q // n_kv
     out, e32, e16 = np.zeros(q.shape), np.zeros(q.shape), np.zeros(q.shape)
     for r in range(n):
-        if row_slot[r] < 0 or pos[r] < 0 or row_slot[r] >= len(table):
+        if row_slot[r] < 0 or pos[r] < 0 or row_slot[r] >= len(table) or pos[r] // PAGE >= table.shape[1]:
             continue
         for g in range(n_kv):
             K, V = [], []
@@ -619,6 +619,53 @@ def test_attention_row_counts(rows):
     sel = random_sel(pos, n_kv, top_k, rows)
     q = randn((rows, n_kv * G, hd), "bf16", 6)
     check_attention(kv, q, table, np.repeat(slots[:1], rows).astype(np.int32), pos, sel)
+
+
+@pytest.mark.parametrize("hd,G", [(128, 1), (64, 2), (128, 3), (128, 4), (64, 8)])
+@pytest.mark.parametrize("kind", ["plain", "nan", "inf", "twice", "mixed"])
+def test_attention_of_rows_that_share_a_slot(hd, G, kind):
+    """A prompt's rows: pages that only some of them select, whose values are
+    infinite or NaN, must not show in the others; a page listed twice by one
+    row; a padding row and rows of another slot between them."""
+    n_kv, top_k, rows = 2, 24, 600
+    lens = [1500, 700]
+    table, slots = scattered(lens, 150, 100, 5)
+    k, v = fill_pages(table, lens, slots, 150, n_kv, hd, "bf16")
+    kv = cache_over(table, 150, n_kv, hd, "bf16", k_pool=k, v_pool=v)
+    pos = np.arange(900, 900 + rows, dtype=np.int32)
+    row_slot = np.repeat(slots[:1], rows).astype(np.int32)
+    sel = np.full((rows, n_kv, top_k), -1, dtype=np.int32)
+    r = np.random.default_rng(G)
+    for i in range(rows):
+        for g in range(n_kv):
+            sel[i, g] = np.sort(r.permutation(40)[:top_k])
+        if i % 16 == 5:
+            sel[i] = -1
+        elif i % 3 == 0:
+            sel[i, :, -1] = pos[i] // PAGE
+    if kind in ("nan", "inf"):
+        page = table[slots[0], 17]
+        (k if kind == "nan" and G % 2 else v)[page, :, 3, 5] = float(kind)
+    elif kind == "twice":
+        sel[7, 1, 2] = sel[7, 1, 9]
+        sel[100:120, 0, :3] = sel[100:120, 0, 3:4]
+    elif kind == "mixed":
+        row_slot[10], row_slot[33] = -1, slots[1]
+        pos[33], pos[50], pos[70] = 650, -1, 100000
+        row_slot[200:203] = len(table)
+    q = randn((rows, n_kv * G, hd), "bf16", 6)
+    got = kv.attend(q, i32(row_slot), i32(pos), i32(sel)).double().cpu().numpy()
+    f = lambda t: t.double().cpu().numpy()  # noqa: E731
+    with np.errstate(invalid="ignore"):
+        ref, e32, e16 = attention_ref(f(kv.k_pool), f(kv.v_pool), f(q), table, row_slot, pos, sel, None)
+        tol = 1.01 * (e32 + e16 + 2.0**-8 * np.abs(ref))
+        bad = ~(np.abs(got - ref) <= tol)
+    if kind in ("nan", "inf"):
+        hit = (sel == 17).any(axis=2).repeat(G, axis=1)                     # [rows, heads]
+        assert hit.any() and not hit.all() and np.isfinite(got[~hit]).all() and not bad[~hit].any()
+        assert not np.isfinite(got[hit]).all(axis=1).any()
+    else:
+        assert not bad.any()
 
 
 # ---------------------------------------------------------------- together
