@@ -2,6 +2,7 @@
 // caller's memory.  They keep nothing between calls and allocate nothing.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <string>
 
 #include "error.hpp"
@@ -113,9 +114,19 @@ bool vectors(const outlets_kv_pages* c, const void* p, int64_t stride) {
     return aligned16(p) && stride % (c->fmt == OUTLETS_FMT_F32 ? 4 : 8) == 0;
 }
 
+// Compute units of a device, asked for once.
 int compute_units(int device) {
+    static std::atomic<int> known[64];
+    if (device < 64) {
+        const int n = known[device].load(std::memory_order_relaxed);
+        if (n) return n;
+    }
     int n = 0;
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess || n < 1) n = 256;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess || n < 1) {
+        (void)hipGetLastError();
+        return 256;
+    }
+    if (device < 64) known[device].store(n, std::memory_order_relaxed);
     return n;
 }
 

@@ -110,6 +110,15 @@ pages_append(PageState s, int n_req, const int32_t* __restrict__ slots, const in
     const int tid = threadIdx.x;
     const int mwords = (s.max_slots + 31) / 32, words = (s.num_pages + 31) / 32;
 
+    // the bitmap's first words, while the requests are looked at (8,192 words:
+    // 262,144 pages)
+    constexpr int KEEP = 8;
+    uint32_t kept[KEEP];
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) {
+        const int i = k * kAppendThreads + tid;
+        kept[k] = i < words ? free_word(s, i) : 0u;
+    }
     for (int i = tid; i < mwords; i += kAppendThreads) marks[i] = 0;
     __syncthreads();
 
@@ -148,9 +157,12 @@ pages_append(PageState s, int n_req, const int32_t* __restrict__ slots, const in
 
     // free pages in all
     int cnt = 0;
-    for (int i = tid; i < words; i += kAppendThreads) cnt += __popc(free_word(s, i));
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) cnt += __popc(kept[k]);
+    for (int i = KEEP * kAppendThreads + tid; i < words; i += kAppendThreads) cnt += __popc(free_word(s, i));
     int zero = 0, n_free, dummy;
     block_scan2(cnt, zero, &n_free, &dummy, red);
+    int done = 0;
     const int rc = any_bad ? OUTLETS_ERR_INVALID_ARG : (N > n_free ? OUTLETS_ERR_OUT_OF_PAGES : OUTLETS_OK);
     if (tid == 0) {
         status[0] = rc;
@@ -165,24 +177,36 @@ pages_append(PageState s, int n_req, const int32_t* __restrict__ slots, const in
         return;
     }
 
-    // the N lowest free pages: ranks by prefix sums over the words
-    int done = 0;
-    for (int c = 0; c < words && done < N; c += kAppendThreads) {
-        const int i = c + tid;
-        uint32_t w = i < words ? free_word(s, i) : 0u;
+    // the N lowest free pages: ranks by prefix sums over the words, then a
+    // lane per bit, so that neighbouring lanes store neighbouring ranks
+    auto take = [&](int c, uint32_t w) {             // words c + tid
         int rank = __popc(w), z = 0, total;
         block_scan2(rank, z, &total, &dummy, red);
         rank += done;
+        const int lane = tid & 63;
+        const uint64_t some = __ballot(w != 0 && rank < N);
+        const int last = some ? 63 - __builtin_clzll(some) : -1;
+        for (int i = 0; i <= last; i += 2) {
+            const int j = i + (lane >> 5), b = lane & 31;
+            const uint32_t x = __shfl(w, j, 64);
+            const int at = __shfl(rank, j, 64) + __popc(x & ((1u << b) - 1u));
+            if ((x >> b & 1u) && at < N) list[at] = (c + (tid & ~63) + j) * 32 + b;
+        }
         if (w && rank < N) {
-            uint32_t left = w;
-            while (left && rank < N) {
-                const int b = __ffs(left) - 1;
-                left &= left - 1;
-                list[rank++] = i * 32 + b;
+            uint32_t left = 0;                       // all taken, or all but those from rank N on
+            if (rank + __popc(w) > N) {
+                left = w;
+                for (int k = rank; k < N; ++k) left &= left - 1;
             }
-            s.free_bits[i] = left;
+            s.free_bits[c + tid] = left;
         }
         done += total;
+    };
+    uint32_t next = kept[0];
+    for (int c = 0; c < words && done < N; c += kAppendThreads) {
+        take(c, next);
+        const int i = c + kAppendThreads + tid;
+        next = i < words ? free_word(s, i) : 0u;
     }
     __syncthreads();
     for (int i = tid; i < n_req; i += kAppendThreads) {
@@ -207,14 +231,15 @@ append_rows(PageState s, int n_req, int n_rows, const AppendReq* __restrict__ re
 
 // One block per request.  Every block checks all slots (a few KB), so that a
 // refused call changes nothing and needs no launch of its own for the check.
-__global__ void __launch_bounds__(256)
+constexpr int kReleaseThreads = 512;
+__global__ void __launch_bounds__(kReleaseThreads)
 pages_release(PageState s, int n, const int32_t* __restrict__ slots, int32_t* __restrict__ status) {
     extern __shared__ uint32_t marks[];
     const int mwords = (s.max_slots + 31) / 32;
-    for (int i = threadIdx.x; i < mwords; i += 256) marks[i] = 0;
+    for (int i = threadIdx.x; i < mwords; i += kReleaseThreads) marks[i] = 0;
     __syncthreads();
     bool bad = false;
-    for (int i = threadIdx.x; i < n; i += 256) {
+    for (int i = threadIdx.x; i < n; i += kReleaseThreads) {
         const int slot = slots[i];
         if (slot >= 0 && slot < s.max_slots) {
             if (atomicOr(&marks[slot >> 5], 1u << (slot & 31)) >> (slot & 31) & 1u) bad = true;
@@ -229,7 +254,7 @@ pages_release(PageState s, int n, const int32_t* __restrict__ slots, int32_t* __
     if (slot < 0) return;
     const int len = min(max(s.seq_len[slot], 0), s.max_seq_len), held = (len + kPage - 1) / kPage;
     int32_t* row = s.page_table + static_cast<int64_t>(slot) * s.max_pages;
-    for (int i = threadIdx.x; i < held; i += 256) {
+    for (int i = threadIdx.x; i < held; i += kReleaseThreads) {
         const int page = row[i];
         if (page >= 0 && page < s.num_pages) atomicOr(&s.free_bits[page >> 5], 1u << (page & 31));
         row[i] = -1;
@@ -260,23 +285,48 @@ template <typename T> __device__ __forceinline__ T block_mean(double sum) {
     return static_cast<T>(static_cast<float>(sum * (1.0 / kPage)));
 }
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Calls of this many rows on: tiles of 32 rows (fewer rows are looked at
+// twice; small calls need the workgroups of 16) and non-temporal stores, for
+// what a call of 32 MB or more leaves in no cache (37,800 rows of 8 heads,
+// 310 MB read and written: 88 us with tiles of 16 rows, 80 with 32, 66 with
+// such stores; a copy of as many bytes takes 61).
+constexpr int kBigWrite = 8192;
+
+template <bool STREAM> __device__ __forceinline__ void put16(void* p, u32x4 x) {
+    if constexpr (STREAM) __builtin_nontemporal_store(x, static_cast<u32x4*>(p));
+    else *static_cast<u32x4*>(p) = x;
+}
+
 // K and V of TR rows and one KV head.  Rows that follow each other in one
 // page are a run; the workgroup that holds a run's first row writes all of
 // it, so a prompt's value pages (transposed: [channel][token]) go out as
-// whole 32-byte rows whatever the tile's alignment to pages.  The keys of a
-// page that a run completes are in LDS (this call's) or in the pool (earlier
-// calls'), so its block key needs no second pass.
+// whole 32-byte rows whatever the tile's alignment to pages.  Keys go from
+// registers to their rows; values, and keys for the block keys, cross LDS,
+// where a wave takes a run.  The keys of a page that a
+// run completes are in LDS (this call's) or in the pool (earlier calls'), so
+// its block key needs no second pass.
 template <typename T, int HD, int TR, bool VEC>
 __global__ void __launch_bounds__(256)
 cache_write(KvPages c, int n_rows, const int32_t* __restrict__ slot_map, const T* __restrict__ k, int64_t ldk,
             const T* __restrict__ v, int64_t ldv) {
     constexpr int EX = TR + kPage - 1;              // the last run may end behind the tile
-    constexpr int VE = 16 / sizeof(T);              // elements of a 16-byte access
+    constexpr bool STREAM = TR > 16;
+    constexpr int VE = VEC ? 16 / sizeof(T) : 1;    // elements of an access to k and v
+    typedef T T2 __attribute__((ext_vector_type(2)));
+    struct alignas(VE * sizeof(T)) Chunk { T e[VE]; };
     __shared__ int sm[EX + 1];                      // slot map of rows r0 - 1 ..
-    __shared__ __attribute__((aligned(16))) T lk[EX][HD];
-    __shared__ __attribute__((aligned(16))) T lv[EX][HD];
+    __shared__ bool own[EX];                        // rows of runs that start in the tile
+    constexpr int TE = 16 / sizeof(T);              // tokens of a 16-byte store to a value page
+    constexpr int LD = HD + TE;                     // rows 4 banks apart: a store's tokens do not meet on one
+    __shared__ __attribute__((aligned(16))) T lk[EX][LD];
+    __shared__ __attribute__((aligned(16))) T lv[EX][LD];
     __shared__ int runs[TR], n_runs;
-    const int r0 = blockIdx.x * TR, g = blockIdx.y, tid = threadIdx.x;
+    // the heads of a tile on one XCD (blocks i and i + 8 share one): rows of
+    // k and v stand far apart, so one head's parts meet on few L2 channels
+    const int y = blockIdx.x / 8, g = y % c.n_kv, r0 = (y / c.n_kv * 8 + blockIdx.x % 8) * TR, tid = threadIdx.x;
+    if (r0 >= n_rows) return;
     const int limit = c.num_pages * kPage;
     if (tid == 0) n_runs = 0;
     for (int i = tid; i <= EX; i += 256) {
@@ -289,52 +339,64 @@ cache_write(KvPages c, int n_rows, const int32_t* __restrict__ slot_map, const T
         const int s = sm[i + 1];
         return s >= 0 && (s % kPage == 0 || sm[i] != s - 1);
     };
-    for (int i = tid; i < TR; i += 256)
-        if (leads(i)) runs[atomicAdd(&n_runs, 1)] = i;
-    const int rows = min(EX, n_rows - r0);
-    if (VEC) {
-        for (int e = tid; e < rows * (HD / VE); e += 256) {
-            const int i = e / (HD / VE), ch = e % (HD / VE) * VE;
-            if (sm[i + 1] < 0) continue;
-            const int64_t r = r0 + i;
-            *reinterpret_cast<uint4*>(&lk[i][ch]) = *reinterpret_cast<const uint4*>(k + r * ldk + g * HD + ch);
-            *reinterpret_cast<uint4*>(&lv[i][ch]) = *reinterpret_cast<const uint4*>(v + r * ldv + g * HD + ch);
-        }
-    } else {
-        for (int e = tid; e < rows * HD; e += 256) {
-            const int i = e / HD, ch = e % HD;
-            if (sm[i + 1] < 0) continue;
-            const int64_t r = r0 + i;
-            lk[i][ch] = k[r * ldk + g * HD + ch];
-            lv[i][ch] = v[r * ldv + g * HD + ch];
-        }
+    for (int i = tid; i < EX; i += 256) {
+        if (i < TR && leads(i)) runs[atomicAdd(&n_runs, 1)] = i;
+        int j = i;                                   // its run's first row, or one before the tile
+        while (j >= 0 && sm[j + 1] >= 0 && !leads(j)) --j;
+        own[i] = sm[i + 1] >= 0 && j >= 0 && j < TR;
     }
     __syncthreads();
-    constexpr int PER = 256 / HD;                    // runs at a time, one thread per channel
-    const int ch = tid % HD;
-    for (int j = tid / HD; j < n_runs; j += PER) {
+    const int rows = min(EX, n_rows - r0);
+    for (int e = tid; e < rows * (HD / VE); e += 256) {
+        const int i = e / (HD / VE), ch = e % (HD / VE) * VE, s = sm[i + 1];
+        if (!own[i]) continue;
+        const int64_t r = r0 + i;
+        const Chunk x = *reinterpret_cast<const Chunk*>(k + r * ldk + g * HD + ch);
+        const Chunk y = *reinterpret_cast<const Chunk*>(v + r * ldv + g * HD + ch);
+        T* kp = static_cast<T*>(c.k_pool) + ((static_cast<int64_t>(s / kPage) * c.n_kv + g) * kPage + s % kPage) * HD;
+        if constexpr (VEC) put16<STREAM>(kp + ch, __builtin_bit_cast(u32x4, x));
+        else *reinterpret_cast<Chunk*>(kp + ch) = x;
+        *reinterpret_cast<Chunk*>(&lk[i][ch]) = x;
+        *reinterpret_cast<Chunk*>(&lv[i][ch]) = y;
+    }
+    __syncthreads();
+    const int lane = tid & 63, ch = lane * 2;
+    for (int j = tid >> 6; j < n_runs; j += 4) {
         const int i0 = runs[j], s0 = sm[i0 + 1], off = s0 % kPage;
         int len = 1;
         while (off + len < kPage && i0 + len < EX && sm[i0 + len + 1] == s0 + len) ++len;
-        const int64_t page = s0 / kPage;
-        T* kp = static_cast<T*>(c.k_pool) + (page * c.n_kv + g) * kPage * HD;
-        T* vp = static_cast<T*>(c.v_pool) + ((page * c.n_kv + g) * HD + ch) * kPage;
-        for (int x = 0; x < len; ++x) kp[(off + x) * HD + ch] = lk[i0 + x][ch];
+        const int64_t page = s0 / kPage, at = (page * c.n_kv + g) * HD;
+        T* vp = static_cast<T*>(c.v_pool) + at * kPage;
         if (len == kPage) {
-            T row[kPage];
+            // neighbouring lanes, neighbouring 16 bytes
+            for (int e = lane; e < HD * kPage / TE; e += 64) {
+                const int vc = e / (kPage / TE), t0 = e % (kPage / TE) * TE;
+                alignas(16) T y[TE];
 #pragma unroll
-            for (int x = 0; x < kPage; ++x) row[x] = lv[i0 + x][ch];
-#pragma unroll
-            for (int x = 0; x < kPage / VE; ++x)
-                reinterpret_cast<uint4*>(vp)[x] = *reinterpret_cast<const uint4*>(row + x * VE);
+                for (int x = 0; x < TE; ++x) y[x] = lv[i0 + t0 + x][vc];
+                put16<STREAM>(vp + e * TE, *reinterpret_cast<const u32x4*>(y));
+            }
         } else {
-            for (int x = 0; x < len; ++x) vp[off + x] = lv[i0 + x][ch];
+            for (int x = 0; x < len; ++x)
+                for (int vc = lane; vc < HD; vc += 64) vp[vc * kPage + off + x] = lv[i0 + x][vc];
         }
+        if (ch >= HD) continue;
         if (c.block_keys && off + len == kPage) {
-            double sum = 0.0;
-            for (int x = 0; x < off; ++x) sum += static_cast<double>(to_f32(kp[x * HD + ch]));
-            for (int x = 0; x < len; ++x) sum += static_cast<double>(to_f32(lk[i0 + x][ch]));
-            static_cast<T*>(c.block_keys)[(page * c.n_kv + g) * HD + ch] = block_mean<T>(sum);
+            // all loads of the keys that stand in the pool at once
+            const T* kp = static_cast<const T*>(c.k_pool) + at * kPage + ch;
+            T2 y[kPage];
+#pragma unroll
+            for (int x = 0; x < kPage; ++x) {
+                if (x < off) y[x] = *reinterpret_cast<const T2*>(kp + x * HD);
+                else y[x] = *reinterpret_cast<const T2*>(&lk[i0 + x - off][ch]);
+            }
+            double a = 0.0, b = 0.0;
+#pragma unroll
+            for (int x = 0; x < kPage; ++x) {
+                a += static_cast<double>(to_f32(y[x][0]));
+                b += static_cast<double>(to_f32(y[x][1]));
+            }
+            *reinterpret_cast<T2*>(static_cast<T*>(c.block_keys) + at + ch) = T2{block_mean<T>(a), block_mean<T>(b)};
         }
     }
 }
@@ -346,13 +408,18 @@ void write_rows(const KvPages& c, int n_rows, const int32_t* slot_map, const voi
     const T* vv = static_cast<const T*>(v);
     const bool vec = (reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % 16 == 0 &&
                      (ldk * sizeof(T)) % 16 == 0 && (ldv * sizeof(T)) % 16 == 0;
+    const bool big = n_rows >= kBigWrite && sizeof(T) == 2;
 #define OUTLETS_WRITE(HD, TR, VEC)                                                                             \
-    hipLaunchKernelGGL((cache_write<T, HD, TR, VEC>), dim3((n_rows + TR - 1) / TR, c.n_kv), dim3(256), 0, st, c, \
+    hipLaunchKernelGGL((cache_write<T, HD, TR, VEC>), dim3((n_rows + 8 * TR - 1) / (8 * TR) * 8 * c.n_kv), dim3(256), 0, st, c, \
                        n_rows, slot_map, kk, ldk, vv, ldv)
     if (c.hd == 128) {
-        if (vec) OUTLETS_WRITE(128, 16, true); else OUTLETS_WRITE(128, 16, false);
+        if (!vec) OUTLETS_WRITE(128, 16, false);
+        else if (big) OUTLETS_WRITE(128, (sizeof(T) == 2 ? 32 : 16), true);
+        else OUTLETS_WRITE(128, 16, true);
     } else {
-        if (vec) OUTLETS_WRITE(64, 16, true); else OUTLETS_WRITE(64, 16, false);
+        if (!vec) OUTLETS_WRITE(64, 16, false);
+        else if (big) OUTLETS_WRITE(64, (sizeof(T) == 2 ? 32 : 16), true);
+        else OUTLETS_WRITE(64, 16, true);
     }
 #undef OUTLETS_WRITE
 }
@@ -409,7 +476,7 @@ void launch_pages_append(const PageState& s, int n_req, const int32_t* slots, co
 
 void launch_pages_release(const PageState& s, int n, const int32_t* slots, int32_t* status, hipStream_t st) {
     const size_t marks = sizeof(uint32_t) * ((s.max_slots + 31) / 32);
-    hipLaunchKernelGGL(pages_release, dim3(std::max(n, 1)), dim3(256), marks, st, s, n, slots, status);
+    hipLaunchKernelGGL(pages_release, dim3(std::max(n, 1)), dim3(kReleaseThreads), marks, st, s, n, slots, status);
 }
 
 void launch_cache_write(const KvPages& c, int n_rows, const int32_t* slot_map, const void* k, int64_t ldk,

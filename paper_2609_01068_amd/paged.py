@@ -16,8 +16,8 @@ memory and streams only.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
+import functools
 from typing import Dict, NamedTuple, Optional
 
 import torch
@@ -51,21 +51,28 @@ def _take(buffers, name, shape, dtype, device, fill=None):
     return t
 
 
-def _check_i32(t, name, n, device):
-    if t.dtype != torch.int32 or t.device != device or t.dim() != 1 or not t.is_contiguous() or (n is not None and len(t) != n):
-        raise TypeError(f"{name} must be a contiguous int32 tensor on {device}" + ("" if n is None else f" of {n} entries"))
+def _check_i32(t, name, n, index):
+    """Data pointer of a contiguous int32 vector (of n entries) on device `index`."""
+    if t.dtype != torch.int32 or t.get_device() != index or t.dim() != 1 or not t.is_contiguous() or \
+            (n is not None and t.shape[0] != n):
+        raise TypeError(f"{name} must be a contiguous int32 tensor on cuda:{index}" +
+                        ("" if n is None else f" of {n} entries"))
     return t.data_ptr()
 
 
-@contextlib.contextmanager
-def _on(device, stream):
-    """The call's stream (its handle for the library); tensors that a call
-    allocates belong to it."""
-    if stream is None:
-        yield torch.cuda.current_stream(device).cuda_stream or None
-    else:
+_current_stream = torch._C._cuda_getCurrentRawStream     # (device index) -> handle, without a Stream object
+
+
+def _on_stream(call):
+    """A method that runs on its `stream` argument: what it allocates then
+    belongs to that stream.  None is the current one."""
+    @functools.wraps(call)
+    def wrapper(self, *args, stream=None, **kw):
+        if stream is None:
+            return call(self, *args, **kw)
         with torch.cuda.stream(stream):
-            yield stream.cuda_stream or None
+            return call(self, *args, **kw)
+    return wrapper
 
 
 def _device(device) -> torch.device:
@@ -87,6 +94,7 @@ class PageTables:
                  buffers: Optional[Dict[str, torch.Tensor]] = None):
         B.lib()
         self.device = _device(device)
+        self._index = self.device.index
         self.num_pages, self.max_slots, self.max_seq_len = num_pages, max_slots, max_seq_len
         self.max_pages = -(-max_seq_len // PAGE)
         self.free_bits = _take(buffers, "free_bits", (-(-num_pages // 32),), torch.int32, self.device)
@@ -98,42 +106,43 @@ class PageTables:
         if not buffers:
             self.reset()
 
-    def reset(self, stream=None) -> None:
-        with _on(self.device, stream) as st:
-            B.check(B.lib().outlets_pages_reset(self._ref, st), "outlets_pages_reset")
+    @_on_stream
+    def reset(self) -> None:
+        B.check(B.lib().outlets_pages_reset(self._ref, _current_stream(self._index)), "outlets_pages_reset")
 
-    def append(self, slots: torch.Tensor, new_tokens: torch.Tensor, n_rows: int, out: Optional[Rows] = None,
-               stream=None) -> Rows:
+    @_on_stream
+    def append(self, slots: torch.Tensor, new_tokens: torch.Tensor, n_rows: int, out: Optional[Rows] = None) -> Rows:
         """Append ``new_tokens[i]`` tokens to slot ``slots[i]`` (-1: padding) and
         lay out their rows, ``n_rows`` at most.  A refused call is reported in
         ``status[0]``, on the device."""
-        n = len(slots)
-        sp, tp = _check_i32(slots, "slots", None, self.device), _check_i32(new_tokens, "new_tokens", n, self.device)
-        with _on(self.device, stream) as st:
-            if out is None:
-                # one allocation, sliced; every part 16 bytes apart or more
-                a, r = -(-(n + 1) // 4) * 4, -(-n_rows // 4) * 4
-                buf = torch.empty(a + 3 * r + 4, dtype=torch.int32, device=self.device)
-                out = Rows(buf[:n + 1], buf[a:a + n_rows], buf[a + r:a + r + n_rows],
-                           buf[a + 2 * r:a + 2 * r + n_rows], buf[a + 3 * r:])
-            else:
-                for t, name, m in zip(out, Rows._fields, (n + 1, n_rows, n_rows, n_rows, 4)):
-                    _check_i32(t, name, m, self.device)
-            need = B.lib().outlets_pages_append_workspace(n, n_rows)
-            ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-            rc = B.lib().outlets_pages_append(self._ref, n, sp, tp, n_rows, out.cu.data_ptr(), out.slot_map.data_ptr(),
-                                              out.positions.data_ptr(), out.row_slot.data_ptr(),
-                                              out.status.data_ptr(), ws.data_ptr() if need else None, need, st)
-        B.check(rc, "outlets_pages_append")
+        n, lib = slots.shape[0], B.lib()
+        sp, tp = _check_i32(slots, "slots", None, self._index), _check_i32(new_tokens, "new_tokens", n, self._index)
+        if out is None:
+            if n_rows < 0:
+                raise ValueError("negative n_rows")
+            buf = torch.empty(3 * n_rows + n + 5, dtype=torch.int32, device=self.device)
+            sm, pos, rs, cu, status = buf.split_with_sizes((n_rows, n_rows, n_rows, n + 1, 4))
+            out, base = Rows(cu, sm, pos, rs, status), buf.data_ptr()
+            ptrs = (base + 12 * n_rows, base, base + 4 * n_rows, base + 8 * n_rows, base + 12 * n_rows + 4 * n + 4)
+        else:
+            ptrs = [_check_i32(t, name, m, self._index)
+                    for t, name, m in zip(out, Rows._fields, (n + 1, n_rows, n_rows, n_rows, 4))]
+        need = lib.outlets_pages_append_workspace(n, n_rows)
+        ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        rc = lib.outlets_pages_append(self._ref, n, sp, tp, n_rows, *ptrs, ws.data_ptr() if need else None, need,
+                                      _current_stream(self._index))
+        if rc:
+            B.check(rc, "outlets_pages_append")
         return out
 
-    def release(self, slots: torch.Tensor, stream=None) -> torch.Tensor:
+    @_on_stream
+    def release(self, slots: torch.Tensor) -> torch.Tensor:
         """Empty slots and free their pages; returns the device status word."""
-        sp = _check_i32(slots, "slots", None, self.device)
-        with _on(self.device, stream) as st:
-            status = torch.empty(1, dtype=torch.int32, device=self.device)
-            rc = B.lib().outlets_pages_release(self._ref, len(slots), sp, status.data_ptr(), st)
-        B.check(rc, "outlets_pages_release")
+        sp = _check_i32(slots, "slots", None, self._index)
+        status = torch.empty(1, dtype=torch.int32, device=self.device)
+        rc = B.lib().outlets_pages_release(self._ref, slots.shape[0], sp, status.data_ptr(), _current_stream(self._index))
+        if rc:
+            B.check(rc, "outlets_pages_release")
         return status
 
 
@@ -148,7 +157,7 @@ class PagedKV:
 
     def __init__(self, tables: PageTables, n_kv: int, head_dim: int, fmt: str = "bf16",
                  buffers: Optional[Dict[str, torch.Tensor]] = None):
-        self.tables, self.device = tables, tables.device
+        self.tables, self.device, self._index = tables, tables.device, tables.device.index
         self.n_kv, self.head_dim, self.fmt, self.dtype = n_kv, head_dim, fmt, _DTYPES[fmt]
         p = tables.num_pages
         shapes = dict(k_pool=(p, n_kv, PAGE, head_dim), v_pool=(p, n_kv, head_dim, PAGE), block_keys=(p, n_kv, head_dim))
@@ -163,66 +172,74 @@ class PagedKV:
 
     def _heads(self, t, name, n, heads):
         """Data pointer and row stride of rows [n, heads, hd], whose rows may stand apart."""
-        if t.dtype != self.dtype or t.device != self.device or tuple(t.shape) != (n, heads, self.head_dim):
-            raise TypeError(f"{name} must be a {self.dtype} tensor of shape {(n, heads, self.head_dim)} on {self.device}")
+        hd = self.head_dim
+        if t.dtype != self.dtype or t.get_device() != self._index or t.shape != (n, heads, hd):
+            raise TypeError(f"{name} must be a {self.dtype} tensor of shape {(n, heads, hd)} on {self.device}")
         row, head, one = t.stride()
-        if one != 1 or (heads > 1 and head != self.head_dim) or (n > 1 and row < heads * self.head_dim):
+        if one != 1 or (heads > 1 and head != hd) or (n > 1 and row < heads * hd):
             raise ValueError(f"the heads of a row of {name} must stand together")
-        return t.data_ptr(), row if n > 1 else max(row, heads * self.head_dim)
+        return t.data_ptr(), row if n > 1 else max(row, heads * hd)
 
-    def write(self, slot_map: torch.Tensor, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
+    @_on_stream
+    def write(self, slot_map: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> None:
         """Store keys and values [n, n_kv, hd] of rows at ``slot_map`` (-1: skip)
         and the block keys of the pages that become full."""
-        n = len(slot_map)
-        mp = _check_i32(slot_map, "slot_map", None, self.device)
+        n = slot_map.shape[0]
+        mp = _check_i32(slot_map, "slot_map", n, self._index)
         kp, ks = self._heads(k, "k", n, self.n_kv)
         vp, vs = self._heads(v, "v", n, self.n_kv)
-        with _on(self.device, stream) as st:
-            rc = B.lib().outlets_cache_write(self._ref, n, mp, kp, ks, vp, vs, st)
-        B.check(rc, "outlets_cache_write")
+        rc = B.lib().outlets_cache_write(self._ref, n, mp, kp, ks, vp, vs, _current_stream(self._index))
+        if rc:
+            B.check(rc, "outlets_cache_write")
 
+    @_on_stream
     def select(self, q: torch.Tensor, row_slot: torch.Tensor, positions: torch.Tensor, top_k: int, sink: int = 1,
-               local: int = 4, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+               local: int = 4, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Pages that each row's attention reads: int32 [n, n_kv, top_k]."""
         n, n_q = q.shape[0], q.shape[1]
+        lib, index = B.lib(), self._index
         qp, qs = self._heads(q, "q", n, n_q)
-        rp, pp = _check_i32(row_slot, "row_slot", n, self.device), _check_i32(positions, "positions", n, self.device)
-        with _on(self.device, stream) as st:
-            shape = (n, self.n_kv, top_k)
-            if out is None:
-                out = torch.empty(shape, dtype=torch.int32, device=self.device)
-            elif tuple(out.shape) != shape or out.dtype != torch.int32 or not out.is_contiguous() or out.device != self.device:
-                raise TypeError(f"out must be a contiguous int32 tensor of shape {shape} on {self.device}")
-            need = 0
-            if self.tables.max_pages > top_k and n:
-                need = B.lib().outlets_block_select_workspace(self._ref, n)
-                if need > _SELECT_WS:
-                    need = max(_SELECT_WS, B.lib().outlets_block_select_workspace(self._ref, 1))
-            ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-            rc = B.lib().outlets_block_select(self._ref, n, rp, pp, qp, qs, n_q, top_k, sink, local, out.data_ptr(),
-                                              ws.data_ptr() if need else None, need, st)
-        B.check(rc, "outlets_block_select")
+        rp, pp = _check_i32(row_slot, "row_slot", n, index), _check_i32(positions, "positions", n, index)
+        shape = (n, self.n_kv, top_k)
+        if out is None:
+            out = torch.empty(shape, dtype=torch.int32, device=self.device)
+        elif out.shape != shape or out.dtype != torch.int32 or not out.is_contiguous() or out.get_device() != index:
+            raise TypeError(f"out must be a contiguous int32 tensor of shape {shape} on {self.device}")
+        need = 0
+        if self.tables.max_pages > top_k and n:
+            need = lib.outlets_block_select_workspace(self._ref, n)
+            if need > _SELECT_WS:
+                need = max(_SELECT_WS, lib.outlets_block_select_workspace(self._ref, 1))
+        ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        rc = lib.outlets_block_select(self._ref, n, rp, pp, qp, qs, n_q, top_k, sink, local, out.data_ptr(),
+                                      ws.data_ptr() if need else None, need, _current_stream(index))
+        if rc:
+            B.check(rc, "outlets_block_select")
         return out
 
+    @_on_stream
     def attend(self, q: torch.Tensor, row_slot: torch.Tensor, positions: torch.Tensor, sel: torch.Tensor,
-               gate: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+               gate: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention [n, n_q, hd] of each row over the pages of ``sel`` (as ``select`` gives them)."""
         n, n_q = q.shape[0], q.shape[1]
+        lib, index = B.lib(), self._index
         qp, qs = self._heads(q, "q", n, n_q)
-        rp, pp = _check_i32(row_slot, "row_slot", n, self.device), _check_i32(positions, "positions", n, self.device)
-        if sel.dim() != 3 or tuple(sel.shape[:2]) != (n, self.n_kv) or sel.dtype != torch.int32 or \
-                not sel.is_contiguous() or sel.device != self.device:
+        rp, pp = _check_i32(row_slot, "row_slot", n, index), _check_i32(positions, "positions", n, index)
+        if sel.dim() != 3 or sel.shape[0] != n or sel.shape[1] != self.n_kv or sel.dtype != torch.int32 or \
+                not sel.is_contiguous() or sel.get_device() != index:
             raise TypeError(f"sel must be a contiguous int32 tensor of shape ({n}, {self.n_kv}, top_k) on {self.device}")
         gp, gs = (None, 0) if gate is None else self._heads(gate, "gate", n, n_q)
-        with _on(self.device, stream) as st:
-            if out is None:
-                out = torch.empty((n, n_q, self.head_dim), dtype=self.dtype, device=self.device)
+        if out is None:
+            out = torch.empty((n, n_q, self.head_dim), dtype=self.dtype, device=self.device)
+            op, os_ = out.data_ptr(), n_q * self.head_dim
+        else:
             op, os_ = self._heads(out, "out", n, n_q)
-            need = B.lib().outlets_block_attention_workspace(self._ref, n, n_q, sel.shape[2])
-            ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-            rc = B.lib().outlets_block_attention(self._ref, n, rp, pp, qp, qs, n_q, sel.data_ptr(), sel.shape[2], gp, gs,
-                                                 op, os_, ws.data_ptr() if need else None, need, st)
-        B.check(rc, "outlets_block_attention")
+        need = lib.outlets_block_attention_workspace(self._ref, n, n_q, sel.shape[2])
+        ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        rc = lib.outlets_block_attention(self._ref, n, rp, pp, qp, qs, n_q, sel.data_ptr(), sel.shape[2], gp, gs, op, os_,
+                                         ws.data_ptr() if need else None, need, _current_stream(index))
+        if rc:
+            B.check(rc, "outlets_block_attention")
         return out
 
 

@@ -179,6 +179,29 @@ def test_every_page_and_no_request():
     assert len(free_pages(pt)) == 33 and pt.seq_len.tolist() == [0] * 5 and pt.page_table.max().item() == -1
 
 
+def test_pools_larger_than_the_kept_words():
+    """More pages than a call holds words of, with holes that leave few free
+    pages here and there."""
+    num = 300001
+    pt = tables(num, 4, num * PAGE)
+    assert pt.append(i32([0]), i32([1 << 20]), 1 << 20).status.tolist() == [0, 1 << 20, 65536, num - 65536]
+    for _ in range(3):
+        assert pt.append(i32([1]), i32([1 << 20]), 1 << 20).status[0].item() == 0
+    assert pt.append(i32([2]), i32([5000]), 5000).status[0].item() == 0
+    r = np.random.default_rng(0)
+    bits = r.integers(0, 2**32, size=-(-num // 32), dtype=np.uint64).astype(np.uint32) & \
+        r.integers(0, 2**32, size=-(-num // 32), dtype=np.uint64).astype(np.uint32)
+    bits[:100] = 0
+    bits[-1] &= (1 << (num % 32)) - 1
+    pt.free_bits.copy_(torch.as_tensor(bits.view(np.int32)))
+    free = sorted(free_pages(pt))
+    rows = pt.append(i32([3, 2]), i32([900000, 9]), 1 << 20)
+    n = 900000 // PAGE + (1 if (5000 + 9 + 15) // PAGE > (5000 + 15) // PAGE else 0)
+    assert rows.status.tolist() == [0, 900009, n, len(free) - n]
+    assert pt.page_table[3, :900000 // PAGE].tolist() == free[:900000 // PAGE]
+    assert sorted(free_pages(pt)) == free[n:]
+
+
 # ---------------------------------------------------------------- cache write
 
 def make_kv(pt, n_kv, hd, fmt, seed=0, scale=1.0):
@@ -250,6 +273,32 @@ def test_cache_write(fmt, hd, n_kv, layout):
         plain_write(ref, sm.tolist(), k, v)
         for a, b, name in zip((kv.k_pool, kv.v_pool, kv.block_keys), ref, ("k", "v", "keys")):
             assert same_bits(a, b), (i, name)
+
+
+@pytest.mark.parametrize("fmt,hd,T", [("bf16", 128, 8192), ("bf16", 64, 9001), ("f32", 128, 9001), ("bf16", 128, 8191)])
+def test_cache_write_of_many_rows(fmt, hd, T):
+    """Around the size where tiles grow: prompts behind partly filled pages."""
+    n_kv, lens = 3, [1, 17, 900, 2900, 40]
+    lens.append(T - sum(lens))
+    pt = tables(700, 6, 9100)
+    kv = make_kv(pt, n_kv, hd, fmt)
+    first = pt.append(i32(range(6)), i32([3, 0, 15, 16, 1, 30]), 65)
+    k0, v0 = randn((65, n_kv, hd), fmt, 1), randn((65, n_kv, hd), fmt, 2)
+    kv.write(first.slot_map, k0, v0)
+    rows = pt.append(i32([4, 1, 0, 5, 2, 3]), i32(lens), T)
+    assert rows.status[0].item() == 0
+    kp, vp, bk = (t.clone() for t in (kv.k_pool, kv.v_pool, kv.block_keys))
+    k, v = randn((T, n_kv, hd), fmt, 3), randn((T, n_kv, hd), fmt, 4)
+    kv.write(rows.slot_map, k, v)
+    at = rows.slot_map.long()
+    kp[at // PAGE, :, at % PAGE], vp[at // PAGE, :, :, at % PAGE] = k, v
+    full = at[at % PAGE == PAGE - 1] // PAGE
+    total = torch.zeros((len(full), n_kv, hd), dtype=torch.float64, device="cuda")
+    for j in range(PAGE):
+        total = total + kp[full, :, j].double()
+    bk[full] = (total / PAGE).float().to(bk.dtype)
+    for a, b in zip((kv.k_pool, kv.v_pool, kv.block_keys), (kp, vp, bk)):
+        assert same_bits(a, b)
 
 
 def test_cache_write_without_block_keys_and_scattered():
