@@ -271,6 +271,25 @@ int outlets_predict_step_noalloc(outlets_ctx* ctx, int32_t n_req, const int32_t*
                                  int64_t row_stride, const int32_t* tokens, float* z_out,
                                  void* hdraft_out, void* stream);
 
+/*
+ * Sparse attention in later decode steps: a step in which some request has
+ * more than top_k pages cached (its token included) attends, per request and
+ * KV head, only to the pages that outlets_block_select would give for
+ * (top_k, sink, local), with the context's queries and cache; the output is
+ * that of outlets_block_attention.  Requests with at most top_k pages still
+ * attend to all of them, and steps in which every request has are those of a
+ * context without sparse attention, bit for bit.  Prefill attends to
+ * everything.  outlets_predict_step_noalloc does the same (its selection and
+ * scores live in the context).  top_k = 0 turns it off.
+ * Allocates the block keys (1/16 of the key pool) and the selection's buffers
+ * and synchronises the device; to be called while no slot is active, since
+ * cached pages have no block keys yet (SLOT_BUSY; turning it off is possible
+ * at any time).  Errors, nothing changed: sink < 0, local < 1 or
+ * sink + local > top_k (INVALID_ARG); more than 16 query heads per KV head
+ * (UNSUPPORTED).  After a failed allocation (NOMEM) it is off.
+ */
+int outlets_sparse_steps(outlets_ctx* ctx, int32_t top_k, int32_t sink, int32_t local);
+
 /* End requests: frees their pages and state.  Inactive slots are a no-op;
  * an out-of-range or repeated slot fails with no change. */
 int outlets_release(outlets_ctx* ctx, int32_t n, const int32_t* slots);
@@ -493,7 +512,9 @@ enum {
     OUTLETS_BUF_POOLED = 9,     /* head input p, float32 [n_req, 2d] */
     OUTLETS_BUF_K_POOL = 10,    /* key pages, act [num_pages, n_kv, 16, hd] */
     OUTLETS_BUF_V_POOL = 11,    /* value pages, transposed: act [num_pages, n_kv, hd, 16] */
-    OUTLETS_BUF_NORM_EMB = 12   /* RMSNorm(embed[token]) * gamma_emb, act [T, d] (input embeddings) */
+    OUTLETS_BUF_NORM_EMB = 12,  /* RMSNorm(embed[token]) * gamma_emb, act [T, d] (input embeddings) */
+    OUTLETS_BUF_BLOCK_KEYS = 13, /* act [num_pages, n_kv, hd] (sparse steps) */
+    OUTLETS_BUF_SELECTED = 14   /* int32 [n_req, n_kv, top_k]: pages of the last call, a sparse step */
 };
 
 /*

@@ -40,7 +40,7 @@ KERNELS = ["META", "FUSE_GEMM", "NORM", "QKV_GEMM", "ROPE_KV", "ATTN", "O_GEMM",
 
 BUF = {name: i for i, name in enumerate(
     ["FUSED", "NORM_ATTN", "Q", "ATTN", "X1", "NORM_MLP", "MLP_ACT", "X2", "HDRAFT",
-     "POOLED", "K_POOL", "V_POOL", "NORM_EMB"])}
+     "POOLED", "K_POOL", "V_POOL", "NORM_EMB", "BLOCK_KEYS", "SELECTED"])}
 
 
 class OutletsError(RuntimeError):
@@ -104,6 +104,7 @@ _SIGS = {
     "outlets_predict_prefill": (C.c_int, [_P, C.c_int32, _I32P, _I32P, _P, _P, _P, C.c_int64, _P, _P, _P, _P]),
     "outlets_predict_step": (C.c_int, [_P, C.c_int32, _I32P, _P, _P, _P, C.c_int64, _P, _P, _P, _P]),
     "outlets_predict_step_noalloc": (C.c_int, [_P, C.c_int32, _I32P, _P, _P, _P, C.c_int64, _P, _P, _P, _P]),
+    "outlets_sparse_steps": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32]),
     "outlets_release": (C.c_int, [_P, C.c_int32, _I32P]),
     "outlets_probe_prefill": (C.c_int, [_P, C.c_int32, _I32P, _I32P, _P, C.c_int64, _P, _P]),
     "outlets_probe_step": (C.c_int, [_P, C.c_int32, _I32P, _P, C.c_int64, _P, _P]),
@@ -216,6 +217,10 @@ def outlets_predict_step_noalloc(ctx, slots, h_low: int, h_mid: int, h_high: int
                                  stream: Optional[int]) -> int:
     return lib().outlets_predict_step_noalloc(ctx, len(slots), i32_array(slots), h_low, h_mid, h_high,
                                               row_stride, tokens, z_out, hdraft_out, stream)
+
+
+def outlets_sparse_steps(ctx, top_k: int, sink: int, local: int) -> int:
+    return lib().outlets_sparse_steps(ctx, top_k, sink, local)
 
 
 def outlets_release(ctx, slots) -> int:

@@ -17,6 +17,7 @@
 #include "error.hpp"
 #include "kernels.hpp"
 #include "outlets.h"
+#include "paged.hpp"
 #include "pager.hpp"
 #include "sched.hpp"
 
@@ -137,6 +138,16 @@ struct outlets_ctx {
     bool decode_by_request = false;   // the current step's attention needs no plan
     int32_t n_tiles = 0;
 
+    // sparse steps (outlets_sparse_steps; top = 0: off)
+    int32_t sparse_top = 0, sparse_sink = 0, sparse_local = 0;
+    bool sparse_now = false;     // the current step's attention is sparse
+    void* block_keys = nullptr;  // [num_pages, n_kv, hd] act
+    int32_t* sparse_sel = nullptr;   // [max_batch_requests, n_kv, sparse_top]
+    void* sparse_ws = nullptr;   // scores of a selection
+    int64_t sparse_ws_bytes = 0;
+    void* sparse_rec = nullptr;  // records of split attention
+    int32_t last_sparse = 0;     // the last call's selection: pages per row and head (0: none)
+
     int32_t* h_stage[2] = {nullptr, nullptr};
     hipEvent_t ev[2] = {nullptr, nullptr};
     bool ev_used[2] = {false, false};
@@ -187,6 +198,21 @@ struct outlets_ctx {
         }
         allocs.push_back(*p);
         return OUTLETS_OK;
+    }
+
+    // Frees one of the allocations (the device is idle) and clears the pointer.
+    template <typename P> void release(P** p) {
+        const auto it = std::find(allocs.begin(), allocs.end(), static_cast<void*>(*p));
+        if (it != allocs.end()) {
+            (void)hipFree(*it);
+            allocs.erase(it);
+        }
+        *p = nullptr;
+    }
+
+    KvPages pages() const {
+        return KvPages{kpool, vpool, block_keys, page_table, act_fmt, cfg.n_kv_heads, cfg.head_dim, cfg.num_pages,
+                       cfg.max_slots, max_pages};
     }
 };
 
@@ -464,10 +490,21 @@ int run_layer(outlets_ctx* c, const CallBufs& b, const MetaFetch& mf, bool prefi
                          c->kpool, c->vpool, c->cos_t, c->sin_t, c->cfg.n_q_heads, c->cfg.n_kv_heads,
                          c->cfg.head_dim, st); }
     }
+    // the block keys of the pages that this call's tokens complete
+    if (c->sparse_top > 0) {
+        KTimer t(c, OUTLETS_K_ROPE_KV, st);
+        launch_block_keys(c->pages(), T, b.tok_slot, b.tok_pos, st);
+    }
     { KTimer t(c, OUTLETS_K_ATTN, st);
       const void* gate = c->gated ? static_cast<const char*>(b.qkv) + (c->qdim + 2 * c->kvdim) * fmt_bytes(af)
                                   : nullptr;
-      if (prefill && c->n_work > 0)
+      if (!prefill && c->sparse_now) {
+          const BlockRows rows{T, b.tok_slot, b.tok_pos, b.qkv, c->qkv_dim, c->cfg.n_q_heads};
+          launch_block_select(c->pages(), rows, c->sparse_top, c->sparse_sink, c->sparse_local, c->sparse_sel,
+                              c->sparse_ws, c->sparse_ws_bytes, gemm_device_cus(), st);
+          launch_block_attention(c->pages(), rows, c->sparse_sel, c->sparse_top, gate, c->qkv_dim, b.attn, c->qdim,
+                                 c->sparse_rec, gemm_device_cus(), st);
+      } else if (prefill && c->n_work > 0)
           launch_attn_prefill(c->n_work, b.d_meta + c->work_off, c->attn_qtile, b.qkv, c->qkv_dim, b.attn, c->qdim,
                               req_off, req_slot, c->page_table, c->max_pages, c->kpool, c->vpool,
                               c->cfg.n_q_heads, c->cfg.n_kv_heads, gate, st);
@@ -726,7 +763,11 @@ int predict_step_impl(outlets_ctx* ctx, bool noalloc, int32_t n_req, const int32
     // per wave and KV head (segments and pieces, see attn_decode_plan)
     DecodePlan plan;
     bool by_request = false;
-    if (attn_prefill_mfma_supported(ctx->act_fmt, ctx->cfg.n_q_heads, ctx->cfg.n_kv_heads, ctx->cfg.head_dim)) {
+    // sparse where some request sees more pages than it would select
+    int32_t longest = 0;
+    for (int i = 0; i < n_req; ++i) longest = std::max(longest, start[i] / 16 + 1);
+    const bool sparse = ctx->sparse_top > 0 && longest > ctx->sparse_top;
+    if (!sparse && attn_prefill_mfma_supported(ctx->act_fmt, ctx->cfg.n_q_heads, ctx->cfg.n_kv_heads, ctx->cfg.head_dim)) {
         std::vector<int32_t> pages(n_req);
         for (int i = 0; i < n_req; ++i) pages[i] = (start[i] + 1 + 15) / 16;
         by_request = attn_decode_by_request(n_req, pages.data(), ctx->cfg.n_kv_heads, gemm_device_cus());
@@ -765,6 +806,7 @@ int predict_step_impl(outlets_ctx* ctx, bool noalloc, int32_t n_req, const int32
     ctx->n_lanes = plan.n_lanes;
     ctx->n_segs = plan.n_segs;
     ctx->decode_by_request = by_request;
+    ctx->sparse_now = sparse;
     NoTiming nt(ctx, noalloc);
     MetaFetch mf{};
     rc = stage_meta(ctx, *bufs, n_req, off, slots, start, updates, plan.work, plan.cu_segs, plan.lanes, 4, &mf, st);
@@ -775,6 +817,7 @@ int predict_step_impl(outlets_ctx* ctx, bool noalloc, int32_t n_req, const int32
     ctx->last_n = n_req;
     ctx->last_T = n_req;
     ctx->last_in_scratch = noalloc;
+    ctx->last_sparse = sparse ? ctx->sparse_top : 0;
     return OUTLETS_OK;
 }
 
@@ -965,6 +1008,44 @@ int outlets_create(const outlets_config* cfg, const outlets_weights* weights, in
     return OUTLETS_OK;
 }
 
+int outlets_sparse_steps(outlets_ctx* ctx, int32_t top_k, int32_t sink, int32_t local) {
+    if (!ctx) return fail(OUTLETS_ERR_INVALID_ARG, "null context");
+    if (top_k == 0) {
+        ctx->sparse_top = 0;
+        return OUTLETS_OK;
+    }
+    if (sink < 0 || local < 1 || top_k < 1 || static_cast<int64_t>(sink) + local > top_k)
+        return fail(OUTLETS_ERR_INVALID_ARG, "needs sink >= 0, local >= 1 and sink + local <= top_k");
+    const outlets_config& cfg = ctx->cfg;
+    if (cfg.n_q_heads / cfg.n_kv_heads > 16)
+        return fail(OUTLETS_ERR_UNSUPPORTED, "more than 16 query heads per KV head");
+    for (int32_t s = 0; s < cfg.max_slots; ++s)
+        if (ctx->pager->seq_len(s) > 0) return fail(OUTLETS_ERR_SLOT_BUSY, "a slot is active");
+    HIP_TRY(hipSetDevice(ctx->device), "hipSetDevice");
+    HIP_TRY(hipDeviceSynchronize(), "hipDeviceSynchronize");
+    ctx->sparse_top = 0;
+    ctx->last_sparse = 0;
+    for (void** p : {&ctx->block_keys, &ctx->sparse_ws, &ctx->sparse_rec}) ctx->release(p);
+    ctx->release(&ctx->sparse_sel);
+    const KvPages c = ctx->pages();
+    const int64_t Bm = cfg.max_batch_requests, eb = static_cast<int64_t>(fmt_bytes(ctx->act_fmt));
+    // selections of large batches go part by part through 256 MiB of scores
+    const int64_t row = block_select_ws(c, 1);
+    ctx->sparse_ws_bytes = std::max(row, std::min<int64_t>(block_select_ws(c, Bm), 256 << 20));
+    int64_t rec = 0;
+    for (int64_t n = 1; n <= Bm; ++n)
+        rec = std::max(rec, block_attention_ws(c, n, cfg.n_q_heads, top_k, gemm_device_cus()));
+    int rc = ctx->alloc(&ctx->block_keys, eb * cfg.num_pages * cfg.n_kv_heads * cfg.head_dim);
+    if (!rc) rc = ctx->alloc(reinterpret_cast<void**>(&ctx->sparse_sel), sizeof(int32_t) * Bm * cfg.n_kv_heads * top_k);
+    if (!rc) rc = ctx->alloc(&ctx->sparse_ws, ctx->sparse_ws_bytes);
+    if (!rc) rc = ctx->alloc(&ctx->sparse_rec, rec);
+    if (rc) return rc;
+    ctx->sparse_sink = sink;
+    ctx->sparse_local = local;
+    ctx->sparse_top = top_k;
+    return OUTLETS_OK;
+}
+
 int outlets_destroy(outlets_ctx* ctx) {
     delete ctx;
     return OUTLETS_OK;
@@ -1021,6 +1102,7 @@ int outlets_predict_prefill(outlets_ctx* ctx, int32_t n_req, const int32_t* slot
     }
     ctx->last_n = n_req;
     ctx->last_T = static_cast<int32_t>(T);
+    ctx->last_sparse = 0;
     ctx->last_in_scratch = false;
     return OUTLETS_OK;
 }
@@ -1255,11 +1337,24 @@ int outlets_get_buffer(outlets_ctx* ctx, int32_t which, void* dst, int64_t nbyte
             size = ab * static_cast<int64_t>(ctx->cfg.num_pages) * ctx->cfg.n_kv_heads * 16 * ctx->cfg.head_dim;
             needs_keep = false;
             break;
+        case OUTLETS_BUF_BLOCK_KEYS:
+            if (!ctx->sparse_top) return fail(OUTLETS_ERR_INVALID_ARG, "sparse steps are off");
+            src = ctx->block_keys;
+            size = ab * static_cast<int64_t>(ctx->cfg.num_pages) * ctx->cfg.n_kv_heads * ctx->cfg.head_dim;
+            needs_keep = false;
+            break;
+        case OUTLETS_BUF_SELECTED:
+            if (!ctx->last_sparse) return fail(OUTLETS_ERR_INVALID_ARG, "the last call's attention was not sparse");
+            src = ctx->sparse_sel;
+            size = static_cast<int64_t>(sizeof(int32_t)) * n * ctx->cfg.n_kv_heads * ctx->last_sparse;
+            needs_keep = false;
+            break;
         default: return fail(OUTLETS_ERR_INVALID_ARG, "unknown buffer id");
     }
     *n_bytes = size;
     if (needs_keep && !keep) return fail(OUTLETS_ERR_INVALID_ARG, "buffer needs keep_intermediates");
-    if (ctx->last_in_scratch && which != OUTLETS_BUF_K_POOL && which != OUTLETS_BUF_V_POOL)
+    if (ctx->last_in_scratch && which != OUTLETS_BUF_K_POOL && which != OUTLETS_BUF_V_POOL &&
+        which != OUTLETS_BUF_BLOCK_KEYS && which != OUTLETS_BUF_SELECTED)
         return fail(OUTLETS_ERR_INVALID_ARG, "the last predict call ran in the static scratch (no-allocation step)");
     if (!dst || nbytes < size) return fail(OUTLETS_ERR_INVALID_ARG, "destination too small");
     HIP_TRY(hipSetDevice(ctx->device), "hipSetDevice");

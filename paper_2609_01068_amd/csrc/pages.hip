@@ -424,21 +424,34 @@ void write_rows(const KvPages& c, int n_rows, const int32_t* slot_map, const voi
 #undef OUTLETS_WRITE
 }
 
-// One wave per row and KV head: rows that end a page average its 16 keys.
+// Rows that end a page average its 16 keys: a wave looks at 64 rows and takes
+// those pages one after another, all of a page's keys in flight.
 template <typename T, int HD>
 __global__ void __launch_bounds__(64)
-block_keys_kernel(KvPages c, const int32_t* __restrict__ row_slot, const int32_t* __restrict__ positions) {
-    const int r = blockIdx.x, g = blockIdx.y;
-    const int pos = positions[r], slot = row_slot[r];
-    if (pos < 0 || pos % kPage != kPage - 1 || slot < 0) return;
-    const int page = c.page_table[static_cast<int64_t>(slot) * c.max_pages + pos / kPage];
-    if (page < 0 || page >= c.num_pages) return;
-    const T* kp = static_cast<const T*>(c.k_pool) + (static_cast<int64_t>(page) * c.n_kv + g) * kPage * HD;
-    for (int ch = threadIdx.x; ch < HD; ch += 64) {
-        double sum = 0.0;
+block_keys_kernel(KvPages c, int n_rows, const int32_t* __restrict__ row_slot, const int32_t* __restrict__ positions) {
+    typedef T T2 __attribute__((ext_vector_type(2)));
+    const int g = blockIdx.x, lane = threadIdx.x, r = blockIdx.y * 64 + lane, ch = 2 * lane;
+    int page = -1;
+    if (r < n_rows) {
+        const int pos = positions[r], slot = row_slot[r];
+        if (pos >= 0 && pos % kPage == kPage - 1 && pos / kPage < c.max_pages && slot >= 0 && slot < c.max_slots)
+            page = c.page_table[static_cast<int64_t>(slot) * c.max_pages + pos / kPage];
+        if (page >= c.num_pages) page = -1;
+    }
+    for (uint64_t todo = __ballot(page >= 0); todo; todo &= todo - 1) {
+        const int64_t at = (static_cast<int64_t>(__shfl(page, __builtin_ctzll(todo), 64)) * c.n_kv + g) * HD + ch;
+        if (ch >= HD) continue;
+        const T* kp = static_cast<const T*>(c.k_pool) + (at - ch) * kPage + ch;
+        T2 y[kPage];
 #pragma unroll
-        for (int x = 0; x < kPage; ++x) sum += static_cast<double>(to_f32(kp[x * HD + ch]));
-        static_cast<T*>(c.block_keys)[(static_cast<int64_t>(page) * c.n_kv + g) * HD + ch] = block_mean<T>(sum);
+        for (int x = 0; x < kPage; ++x) y[x] = *reinterpret_cast<const T2*>(kp + x * HD);
+        double a = 0.0, b = 0.0;
+#pragma unroll
+        for (int x = 0; x < kPage; ++x) {
+            a += static_cast<double>(to_f32(y[x][0]));
+            b += static_cast<double>(to_f32(y[x][1]));
+        }
+        *reinterpret_cast<T2*>(static_cast<T*>(c.block_keys) + at) = T2{block_mean<T>(a), block_mean<T>(b)};
     }
 }
 
@@ -489,14 +502,15 @@ void launch_cache_write(const KvPages& c, int n_rows, const int32_t* slot_map, c
 void launch_block_keys(const KvPages& c, int n_rows, const int32_t* row_slot, const int32_t* positions,
                        hipStream_t st) {
     if (n_rows <= 0) return;
-    const dim3 grid(n_rows, c.n_kv), block(64);
+    const dim3 grid(c.n_kv, (n_rows + 63) / 64), block(64);
+#define OUTLETS_KEYS(T, HD) \
+    hipLaunchKernelGGL((block_keys_kernel<T, HD>), grid, block, 0, st, c, n_rows, row_slot, positions)
     if (c.fmt == OUTLETS_FMT_F32) {
-        if (c.hd == 128) hipLaunchKernelGGL((block_keys_kernel<float, 128>), grid, block, 0, st, c, row_slot, positions);
-        else hipLaunchKernelGGL((block_keys_kernel<float, 64>), grid, block, 0, st, c, row_slot, positions);
+        if (c.hd == 128) OUTLETS_KEYS(float, 128); else OUTLETS_KEYS(float, 64);
     } else {
-        if (c.hd == 128) hipLaunchKernelGGL((block_keys_kernel<__bf16, 128>), grid, block, 0, st, c, row_slot, positions);
-        else hipLaunchKernelGGL((block_keys_kernel<__bf16, 64>), grid, block, 0, st, c, row_slot, positions);
+        if (c.hd == 128) OUTLETS_KEYS(__bf16, 128); else OUTLETS_KEYS(__bf16, 64);
     }
+#undef OUTLETS_KEYS
 }
 
 }  // namespace outlets

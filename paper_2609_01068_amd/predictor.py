@@ -163,6 +163,13 @@ class OutletsPredictor:
         B.check(rc, "outlets_predict_step_noalloc" if noalloc else "outlets_predict_step")
         return z_out[:n], (hdraft_out[:n] if hdraft_out is not None else None)
 
+    def sparse_steps(self, top_k: int, sink: int = 1, local: int = 4) -> None:
+        """Let later steps attend to ``top_k`` pages of 16 tokens per request and
+        KV head at most (0: to everything), the first ``sink``, the last
+        ``local`` and those whose block keys score highest.  Call it while no
+        slot is active."""
+        B.check(B.outlets_sparse_steps(self.ctx, top_k, sink, local), "outlets_sparse_steps")
+
     def release(self, slots: Sequence[int]) -> None:
         B.check(B.outlets_release(self.ctx, list(slots)), "outlets_release")
 
