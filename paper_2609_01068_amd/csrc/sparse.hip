@@ -230,12 +230,8 @@ __device__ __forceinline__ int wave_inclusive(int v) {
     return v;
 }
 
-// Order-preserving maps of scores to unsigned keys; -0 counts as +0 and, in
-// 64 bits, NaN as -infinity.
-__device__ __forceinline__ uint32_t order_key(float s) {
-    const uint32_t u = __float_as_uint(s + 0.f);
-    return u ^ ((u >> 31) ? ~0u : (1u << 31));
-}
+// Order-preserving map of a score to an unsigned key above 0; -0 counts as +0
+// and NaN as -infinity.
 __device__ __forceinline__ uint64_t order_key(double s) {
     if (s != s) s = -__builtin_inf();
     const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
@@ -262,32 +258,31 @@ template <int NT>
 struct PickShared {
     static constexpr int kNear = near_cap(NT);
     int hist[256];
-    int red[NT / 64][2];
+    int red[NT / 64];
     float fred[NT / 64][2];
-    float value[kNear];
     int index[kNear];
     double exact[kNear];
-    uint64_t prefix;
-    int bin, want, count, n;
+    int bin, want, n, in, near;
     float t;
 };
 
-// Sums of a and b over the group, in every thread.
+// Sum over the group, in every thread.
 template <int NT>
-__device__ __forceinline__ int2 block_sum2(int a, int b, PickShared<NT>& sh) {
+__device__ __forceinline__ int block_sum(int a, PickShared<NT>& sh) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) { a += __shfl_xor(a, o, 64); b += __shfl_xor(b, o, 64); }
-    if (NT == 64) return make_int2(a, b);
-    if ((threadIdx.x & 63) == 0) { sh.red[threadIdx.x >> 6][0] = a; sh.red[threadIdx.x >> 6][1] = b; }
+    for (int o = 32; o > 0; o >>= 1) a += __shfl_xor(a, o, 64);
+    if (NT > 64 && (threadIdx.x & 63) == 0) sh.red[threadIdx.x >> 6] = a;
     group_sync<NT>();
-    int2 t = make_int2(0, 0);
-    for (int i = 0; i < NT / 64; ++i) { t.x += sh.red[i][0]; t.y += sh.red[i][1]; }
+    if (NT == 64) return a;
+    a = 0;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) a += sh.red[i];
     group_sync<NT>();
-    return t;
+    return a;
 }
 
 // The histogram's bin (largest first) that holds the want-th entry: sh.bin,
-// the rank within it in sh.want and its size in sh.count.
+// the rank within it in sh.want.
 template <int NT>
 __device__ __forceinline__ void find_bin(int want, PickShared<NT>& sh) {
     if (NT == 64 || threadIdx.x < 64) {
@@ -301,7 +296,6 @@ __device__ __forceinline__ void find_bin(int want, PickShared<NT>& sh) {
                 if (before + h[j] >= want) {
                     sh.bin = 255 - 4 * lane - j;
                     sh.want = want - before;
-                    sh.count = h[j];
                     break;
                 }
                 before += h[j];
@@ -311,24 +305,23 @@ __device__ __forceinline__ void find_bin(int want, PickShared<NT>& sh) {
     group_sync<NT>();
 }
 
-// The want-th largest key of those that key(i, k) names for i in [lo, hi), by
-// eight bits at a time; *left receives how many keys equal to it are wanted.
-template <int NT, typename K, typename F>
-__device__ __forceinline__ K radix_select(int lo, int hi, int want, F key, int* left, PickShared<NT>& sh) {
+// The want-th largest of keys [lo, hi), by eight bits at a time; *left receives
+// how many keys equal to it are wanted.
+template <int NT>
+__device__ __forceinline__ uint64_t radix_select(const uint64_t* keys, int lo, int hi, int want, int* left,
+                                                 PickShared<NT>& sh) {
     const int tid = threadIdx.x % NT;
-    K prefix = 0;
-    constexpr int top = 8 * sizeof(K) - 8;
-    for (int shift = top; shift >= 0; shift -= 8) {
+    uint64_t prefix = 0;
+    for (int shift = 56; shift >= 0; shift -= 8) {
         for (int i = tid; i < 256; i += NT) sh.hist[i] = 0;
         group_sync<NT>();
         for (int i = lo + tid; i < hi; i += NT) {
-            K k;
-            if (key(i, k) && (shift == top || (k >> (shift + 8)) == (prefix >> (shift + 8))))
-                atomicAdd(&sh.hist[(k >> shift) & 255], 1);
+            const uint64_t k = keys[i];
+            if (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&sh.hist[(k >> shift) & 255], 1);
         }
         group_sync<NT>();
         find_bin<NT>(want, sh);
-        prefix |= static_cast<K>(sh.bin) << shift;
+        prefix |= static_cast<uint64_t>(sh.bin) << shift;
         want = sh.want;
         group_sync<NT>();
     }
@@ -336,7 +329,8 @@ __device__ __forceinline__ K radix_select(int lo, int hi, int want, F key, int* 
     return prefix;
 }
 
-// 64-bit score of one page by 16 lanes; every one of them gets it.
+// 64-bit score of one page by 16 lanes; every one of them gets it.  Four
+// heads' queries are in flight at a time.
 template <typename T, int HD>
 __device__ __forceinline__ double exact_score(const KvPages& c, const T* q, int G, int g, int page) {
     double s = -__builtin_inf();
@@ -344,27 +338,68 @@ __device__ __forceinline__ double exact_score(const KvPages& c, const T* q, int 
     constexpr int CH = HD / 16;
     const int at = (threadIdx.x & 15) * CH;
     const T* kb = static_cast<const T*>(c.block_keys) + (static_cast<int64_t>(page) * c.n_kv + g) * HD + at;
-    for (int h = 0; h < G; ++h) {
-        double a = 0.0;
+    T k[CH];
 #pragma unroll
-        for (int e = 0; e < CH; ++e) a = fma(to_f64(kb[e]), to_f64(q[h * HD + at + e]), a);
+    for (int e = 0; e < CH; ++e) k[e] = kb[e];
+    for (int h0 = 0; h0 < G; h0 += 4) {
+        T x[4][CH];
 #pragma unroll
-        for (int o = 1; o < 16; o <<= 1) a += __shfl_xor(a, o, 64);
-        s = a > s ? a : s;                           // NaN: never larger
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < CH; ++e) x[j][e] = q[min(h0 + j, G - 1) * HD + at + e];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            double a = 0.0;
+#pragma unroll
+            for (int e = 0; e < CH; ++e) a = fma(to_f64(k[e]), to_f64(x[j][e]), a);
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) a += __shfl_xor(a, o, 64);
+            s = a > s ? a : s;                       // NaN: never larger
+        }
     }
     return s;
 }
 
+// The scores of a row, dealt to the waves of a group in contiguous parts.
+// Loops over them stay loops: a selection is a dozen short passes, and
+// unrolled over scores held in registers their code did not fit the
+// instruction cache (3,328 selections of 1,650 pages 35 -> 71 us).
+template <int NT>
+struct RowScores {
+    float* sc;
+    int first, end;            // the wave's pages
+
+    __device__ __forceinline__ RowScores(float* scores, int nb) : sc(scores) {
+        const int part = (nb + NT - 1) / NT * 64;
+        first = (threadIdx.x % NT >> 6) * part;
+        end = min(first + part, nb);
+    }
+    // f(page, score) for every page of the wave's part and some behind it, all
+    // lanes together; U scores in flight (1 where the pass is rare)
+    template <int U = 4, typename F> __device__ __forceinline__ void each(F f) const {
+        const int lane = threadIdx.x & 63;
+        for (int i = first + lane; i - lane < end; i += 64 * U) {
+            float v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = sc[min(i + 64 * u, end - 1)];
+#pragma unroll
+            for (int u = 0; u < U; ++u) f(i + 64 * u, v[u]);
+        }
+    }
+};
+
 // The selection of one row and KV head from its scores: pages below `lo`, from
-// `hi` on and the `want` best between them, ascending.  Overwrites scores of
-// the pages that were compared in 64 bits.  By the NT threads of a group.
+// `hi` on and the `want` best between them, ascending.  By the NT threads of a
+// group.
 template <typename T, int HD, int NT>
 __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, float bound, uint64_t* keys,
                          PickShared<NT>& sh) {
     const int tid = threadIdx.x % NT, lane = tid & 63, w = tid >> 6;
-    constexpr int kNear = PickShared<NT>::kNear;
+    constexpr int kNear = PickShared<NT>::kNear, NW = NT / 64;
     const int lo = a.sink, hi = nb - a.local, want = a.top_k - a.sink - a.local;
     int32_t* sel = a.sel + (static_cast<int64_t>(r) * a.c.n_kv + g) * a.top_k;
+    const RowScores<NT> row(sc, nb);
+    auto among = [&](int i) { return i >= lo && i < hi && i < row.end; };
     const float d2 = bound * kScoreErr2 + kScoreErrAbs;
     float thr = INFINITY;                            // pages of at least this score are taken
     if (want > 0) {
@@ -372,15 +407,14 @@ __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, f
         float upper = 0.f, lower = 0.f;
         int need = want, crowd = hi - lo;            // of `crowd` pages near the border, `need` are taken
         if (bounded) {
-            // the want-th largest score: 256 bins between the extremes (a bin
-            // of a linear scale holds few pages, a bin of the first bits
-            // most), then by comparison within its bin
+            // the want-th largest score t, to one of 256 bins between the
+            // extremes (of a linear scale: its bins hold few pages each)
             float mn = INFINITY, mx = -INFINITY;
-            for (int i = lo + tid; i < hi; i += NT) {
-                const float s = sc[i];
+            row.each([&](int i, float s) {
+                if (!among(i)) return;
                 mx = fmaxf(mx, s);
                 if (s > -INFINITY) mn = fminf(mn, s);
-            }
+            });
 #pragma unroll
             for (int o = 32; o > 0; o >>= 1) {
                 mx = fmaxf(mx, __shfl_xor(mx, o, 64));
@@ -390,128 +424,131 @@ __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, f
             for (int i = tid; i < 256; i += NT) sh.hist[i] = 0;
             if (tid == 0) sh.n = 0;
             group_sync<NT>();
-            for (int i = 0; i < NT / 64; ++i) { mx = fmaxf(mx, sh.fred[i][0]); mn = fminf(mn, sh.fred[i][1]); }
+#pragma unroll
+            for (int i = 0; i < NW; ++i) { mx = fmaxf(mx, sh.fred[i][0]); mn = fminf(mn, sh.fred[i][1]); }
             const float scale = mx > mn ? 255.f / (mx - mn) : 0.f;
             auto bin = [&](float s) {                // nondecreasing in s
                 return s > mn ? min(static_cast<int>((s - mn) * scale), 255) : 0;
             };
-            for (int i = lo + tid; i < hi; i += NT) atomicAdd(&sh.hist[bin(sc[i])], 1);
+            row.each([&](int i, float s) {
+                if (among(i)) atomicAdd(&sh.hist[bin(s)], 1);
+            });
             group_sync<NT>();
             find_bin<NT>(want, sh);
-            float t;
-            if (sh.count <= kNear) {
-                const int B = sh.bin, rank = sh.want - 1, n = sh.count;
-                for (int i = lo + tid; i < hi; i += NT) {
-                    const float s = sc[i];
-                    if (bin(s) == B) sh.value[atomicAdd(&sh.n, 1)] = s;
+            // that score t lies in bin B, in [lower + d2, upper - d2] (bin edges,
+            // a hundredth of a bin apart to cover their rounding): pages above
+            // t + d2 are in, pages below t - d2 are not, and both hold for
+            // `upper` and `lower` (with d2 twice a score's error)
+            const float B = static_cast<float>(sh.bin), width = (mx - mn) / 255.f;
+            upper = mn + (B + 1.01f) * width + d2;
+            lower = sh.bin == 0 ? -INFINITY : mn + (B - 0.01f) * width - d2;
+            int in = 0, crowded = 0;
+            row.each([&](int i, float s) {
+                const bool is_in = among(i) && s > upper, close = among(i) && s >= lower && !is_in;
+                in += is_in;
+                if (close) {
+                    const int k = atomicAdd(&sh.n, 1);
+                    if (k < kNear) sh.index[k] = i;
                 }
-                group_sync<NT>();
-                for (int i = tid; i < n; i += NT) {
-                    const float v = sh.value[i];
-                    int above = 0;
-                    for (int j = 0; j < n; ++j) above += sh.value[j] > v || (sh.value[j] == v && j < i);
-                    if (above == rank) sh.t = v;
-                }
-                group_sync<NT>();
-                t = sh.t;
-            } else {
-                int left;
-                const uint32_t k = radix_select<NT, uint32_t>(
-                    lo, hi, want, [&](int i, uint32_t& k) { k = order_key(sc[i]); return true; }, &left, sh);
-                t = __uint_as_float(k ^ ((k >> 31) ? (1u << 31) : ~0u));
-            }
-            upper = t + d2;
-            lower = t - d2;
-            int in = 0, near = 0;
-            for (int i = lo + tid; i < hi; i += NT) {
-                const float s = sc[i];
-                in += s > upper;
-                near += s >= lower && !(s > upper);
-            }
-            const int2 sum = block_sum2<NT>(in, near, sh);
-            need = want - sum.x;
-            crowd = sum.y;
+            });
+            need = want - block_sum<NT>(in, sh);
+            crowd = sh.n;
         }
         if (bounded && need == crowd) {
             thr = lower;
         } else {
-            // the 64-bit scores of the crowd decide, ties by the page index
-            auto near = [&](int i) { return !bounded || (sc[i] >= lower && !(sc[i] > upper)); };
+            // 64-bit scores decide where 32 bits do not, ties by the page index
             const T* q = static_cast<const T*>(a.q) + r * a.ldq + static_cast<int64_t>(g) * a.G * HD;
-            const int32_t* row = a.c.page_table + static_cast<int64_t>(a.row_slot[r]) * a.c.max_pages;
+            const int32_t* table = a.c.page_table + static_cast<int64_t>(a.row_slot[r]) * a.c.max_pages;
             thr = bounded ? fmaxf(upper, -__FLT_MAX__) : 0.f;
-            if (crowd <= kNear) {
-                if (tid == 0) sh.n = 0;
-                group_sync<NT>();
-                for (int i = lo + tid; i < hi; i += NT)
-                    if (near(i)) sh.index[atomicAdd(&sh.n, 1)] = i;
-                group_sync<NT>();
-                for (int i = tid / 16; i < crowd; i += NT / 16) {
-                    const double s = exact_score<T, HD>(a.c, q, a.G, g, row[sh.index[i]]);
-                    if (tid % 16 == 0) sh.exact[i] = s;
-                }
-                group_sync<NT>();
+            if (bounded && crowd <= kNear) {
+                // t itself: the need-th largest of the crowd's 32-bit scores
+                if (tid == 0) sh.in = sh.near = 0;
                 for (int i = tid; i < crowd; i += NT) {
-                    const double s = sh.exact[i];
+                    const float s = sc[sh.index[i]];
                     int above = 0;
-                    for (int j = 0; j < crowd; ++j)
-                        above += sh.exact[j] > s || (sh.exact[j] == s && sh.index[j] < sh.index[i]);
-                    sc[sh.index[i]] = above < need ? INFINITY : -INFINITY;
+                    for (int j = 0; j < crowd; ++j) {
+                        const float x = sc[sh.index[j]];
+                        above += x > s || (x == s && j < i);
+                    }
+                    if (above == need - 1) sh.t = s;
                 }
                 group_sync<NT>();
+                const float t = sh.t;
+                for (int i = tid; i < crowd; i += NT) {
+                    const float s = sc[sh.index[i]];
+                    if (s > t + d2) atomicAdd(&sh.in, 1);
+                    else if (s >= t - d2) atomicAdd(&sh.near, 1);
+                }
+                group_sync<NT>();
+                if (need - sh.in == sh.near) {       // no page that stays out is as near as the error
+                    thr = t - d2;
+                } else {
+                    for (int i = tid / 16; i < crowd; i += NT / 16) {
+                        const double s = exact_score<T, HD>(a.c, q, a.G, g, table[sh.index[i]]);
+                        if (tid % 16 == 0) sh.exact[i] = s;
+                    }
+                    group_sync<NT>();
+                    for (int i = tid; i < crowd; i += NT) {
+                        const double s = sh.exact[i];
+                        int above = 0;
+                        for (int j = 0; j < crowd; ++j)
+                            above += sh.exact[j] > s || (sh.exact[j] == s && sh.index[j] < sh.index[i]);
+                        sc[sh.index[i]] = above < need ? INFINITY : -INFINITY;
+                    }
+                    group_sync<NT>();
+                }
             } else {
+                // keys of all candidates in memory, 0 for those that do not compete
+                row.template each<1>([&](int i, float s) {
+                    if (among(i)) keys[i] = !bounded || (s >= lower && !(s > upper));
+                });
+                __threadfence_block();
+                group_sync<NT>();
                 for (int i = lo + tid / 16; i < hi; i += NT / 16) {
-                    if (!near(i)) continue;
-                    const double s = exact_score<T, HD>(a.c, q, a.G, g, row[i]);
+                    if (!keys[i]) continue;
+                    const double s = exact_score<T, HD>(a.c, q, a.G, g, table[i]);
                     if (tid % 16 == 0) keys[i] = order_key(s);
                 }
                 __threadfence_block();
                 group_sync<NT>();
                 int left;
-                const uint64_t k = radix_select<NT, uint64_t>(
-                    lo, hi, need, [&](int i, uint64_t& k) { if (!near(i)) return false; k = keys[i]; return true; },
-                    &left, sh);
+                const uint64_t k = radix_select<NT>(keys, lo, hi, need, &left, sh);
+                // ties in page order: first those of the waves before
                 int ties = 0;
-                for (int i0 = lo; i0 < hi; i0 += NT) {
-                    const int i = i0 + tid;
-                    const bool mine = i < hi && near(i);
-                    const uint64_t x = mine ? keys[i] : 0;
-                    const bool tie = mine && x == k;
-                    const uint64_t tb = __ballot(tie);
-                    if (lane == 0) sh.red[w][0] = __popcll(tb);
-                    group_sync<NT>();
-                    int t0 = ties;
-                    for (int j = 0; j < NT / 64; ++j) {
-                        if (j < w) t0 += sh.red[j][0];
-                        ties += sh.red[j][0];
-                    }
-                    if (mine) {
-                        const bool take = x > k || (tie && t0 + __popcll(tb & ((1ull << lane) - 1)) < left);
-                        sc[i] = take ? INFINITY : -INFINITY;
-                    }
-                    group_sync<NT>();
-                }
+                row.template each<1>([&](int i, float) { ties += __popcll(__ballot(among(i) && keys[i] == k)); });
+                if (lane == 0) sh.red[w] = ties;
+                group_sync<NT>();
+                ties = 0;
+                for (int j = 0; j < w; ++j) ties += sh.red[j];
+                row.template each<1>([&](int i, float) {
+                    const bool mine = among(i) && keys[i] != 0;
+                    const uint64_t x = mine ? keys[i] : 0, tb = __ballot(mine && x == k);
+                    if (mine)
+                        sc[i] = x > k || (x == k && ties + __popcll(tb & ((1ull << lane) - 1)) < left) ? INFINITY : -INFINITY;
+                    ties += __popcll(tb);
+                });
+                group_sync<NT>();
             }
         }
     }
-    // each wave lists a contiguous part, behind those of the waves before it
-    constexpr int NW = NT / 64;
-    const int part = (nb + NT - 1) / NT * 64, b0 = w * part, b1 = min(b0 + part, nb);
-    auto takes = [&](int b) { return b < b1 && (b < lo || b >= hi || (want > 0 && sc[b] >= thr)); };
+    // each wave lists its part, behind those of the waves before it
+    auto takes = [&](int i, float s) { return i < row.end && (i < lo || i >= hi || (want > 0 && s >= thr)); };
     int at = 0;
     if (NW > 1) {
         int n = 0;
-        for (int b = b0; b < b1; b += 64) n += __popcll(__ballot(takes(b + lane)));
-        if (lane == 0) sh.red[w][0] = n;
+        row.each([&](int i, float s) { n += __popcll(__ballot(takes(i, s))); });
+        if (lane == 0) sh.red[w] = n;
         group_sync<NT>();
-        for (int j = 0; j < w; ++j) at += sh.red[j][0];
+#pragma unroll
+        for (int j = 0; j < NW; ++j) at += j < w ? sh.red[j] : 0;
     }
-    for (int b = b0; b < b1; b += 64) {
-        const bool take = takes(b + lane);
+    row.each([&](int i, float s) {
+        const bool take = takes(i, s);
         const uint64_t m = __ballot(take);
-        if (take) sel[at + __popcll(m & ((1ull << lane) - 1))] = b + lane;
+        if (take) sel[at + __popcll(m & ((1ull << lane) - 1))] = i;
         at += __popcll(m);
-    }
+    });
     group_sync<NT>();
 }
 
@@ -522,6 +559,7 @@ __device__ __forceinline__ void pick_all(const SelectArgs& a, int r, int g, int 
     for (int i = threadIdx.x % NT; i < a.top_k; i += NT) sel[i] = i < nb ? i : -1;
 }
 
+constexpr int kFusedPages = 1024;    // tables up to this many pages take the fused form
 constexpr int kPickLdsPages = 12288; // scores of a row that the split form copies to LDS (48 KB)
 constexpr int kUnit = 64;            // pages that a wave scores at a time
 
@@ -591,15 +629,15 @@ block_scores(SelectArgs a) {
         a.bounds[(static_cast<int64_t>(r + threadIdx.x) * a.c.n_kv + g) * slices + blockIdx.x] = __uint_as_float(big);
 }
 
-template <typename T, int HD, bool LDS, int kPickThreads>
-__global__ void __launch_bounds__(kPickThreads)
+template <typename T, int HD, int NT, bool LDS>
+__global__ void __launch_bounds__(NT)
 block_pick(SelectArgs a, int slices) {
     extern __shared__ float lds[];                   // [max_pages]
-    __shared__ PickShared<kPickThreads> sh;
+    __shared__ PickShared<NT> sh;
     __shared__ uint32_t bound;
     const int g = blockIdx.x, r = blockIdx.y, nb = visible_pages(a, r);
     if (nb <= a.top_k) {
-        pick_all<kPickThreads>(a, r, g, nb);
+        pick_all<NT>(a, r, g, nb);
         return;
     }
     const int64_t item = static_cast<int64_t>(r) * a.c.n_kv + g;
@@ -608,24 +646,23 @@ block_pick(SelectArgs a, int slices) {
     __syncthreads();
     if (LDS) {
         // eight loads in flight: other XCDs wrote the scores, each is a trip to memory
-        for (int i0 = threadIdx.x; i0 < nb; i0 += 8 * kPickThreads) {
+        for (int i0 = threadIdx.x; i0 < nb; i0 += 8 * NT) {
             float v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = sc[min(i0 + k * kPickThreads, nb - 1)];
+            for (int k = 0; k < 8; ++k) v[k] = sc[min(i0 + k * NT, nb - 1)];
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                if (i0 + k * kPickThreads < nb) lds[i0 + k * kPickThreads] = v[k];
+                if (i0 + k * NT < nb) lds[i0 + k * NT] = v[k];
         }
     }
-    for (int i = threadIdx.x; i < slices; i += kPickThreads) {
+    for (int i = threadIdx.x; i < slices; i += NT) {
         const uint32_t b = __float_as_uint(a.bounds[item * slices + i]);
         if (b) atomicMax(&bound, b);
     }
     __syncthreads();
-    if constexpr (LDS)
-        pick_row<T, HD, kPickThreads>(a, r, g, nb, lds, __uint_as_float(bound), a.keys + item * a.c.max_pages, sh);
-    else
-        pick_row<T, HD, kPickThreads>(a, r, g, nb, sc, __uint_as_float(bound), a.keys + item * a.c.max_pages, sh);
+    uint64_t* keys = a.keys + item * a.c.max_pages;
+    if constexpr (LDS) pick_row<T, HD, NT>(a, r, g, nb, lds, __uint_as_float(bound), keys, sh);
+    else pick_row<T, HD, NT>(a, r, g, nb, sc, __uint_as_float(bound), keys, sh);
 }
 
 // ---------------------------------------------------------------- attention
@@ -1110,9 +1147,7 @@ int64_t block_select_ws(const KvPages& c, int64_t n_rows) {
     return n_rows * ((row + 15) / 16 * 16);
 }
 
-// Tables up to this many pages take the fused form.
-constexpr int kFusedPages = 1024;
-constexpr int kFusedBytes = 16 << 10;    // LDS of a block's scores there
+constexpr int kFusedBytes = 16 << 10;    // LDS of a block's scores in the fused form
 
 void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int sink, int local, int32_t* sel, void* ws,
                          int64_t ws_bytes, int cus, hipStream_t st) {
@@ -1149,16 +1184,17 @@ void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int
         } else {                                                                                                  \
             hipLaunchKernelGGL((block_scores<T, HD, GP>), dim3(slices, c.n_kv, n), dim3(64), 0, st, a); \
             if (items < cus) OUTLETS_PICK(T, HD, 1024);                                                            \
-            else OUTLETS_PICK(T, HD, 256);                                                                         \
+            else if (items < 4 * cus) OUTLETS_PICK(T, HD, 256);                                                    \
+            else OUTLETS_PICK(T, HD, 64);                                                                          \
         }                                                                                                         \
     } while (0)
 #define OUTLETS_PICK(T, HD, NT)                                                                                   \
     do {                                                                                                          \
         if (c.max_pages <= kPickLdsPages)                                                                         \
-            hipLaunchKernelGGL((block_pick<T, HD, true, NT>), dim3(c.n_kv, n), dim3(NT), sizeof(float) * c.max_pages, st, \
+            hipLaunchKernelGGL((block_pick<T, HD, NT, true>), dim3(c.n_kv, n), dim3(NT), sizeof(float) * c.max_pages, st, \
                                a, slices);                                                                        \
         else                                                                                                      \
-            hipLaunchKernelGGL((block_pick<T, HD, false, NT>), dim3(c.n_kv, n), dim3(NT), 0, st, a, slices);          \
+            hipLaunchKernelGGL((block_pick<T, HD, NT, false>), dim3(c.n_kv, n), dim3(NT), 0, st, a, slices);          \
     } while (0)
 #define OUTLETS_SELECT_G(HD)                                                                                      \
     switch (gp) {                                                                                                 \
