@@ -669,8 +669,6 @@ block_pick(SelectArgs a, int slices) {
 // Largest query heads per KV head: the columns of a 16-wide MFMA.
 constexpr int kMaxGroup = 16;
 
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-
 constexpr int kAttendWaves = 4;
 
 // What the attention kernels share: the queries' rows, the selection and
@@ -768,61 +766,81 @@ __global__ void __launch_bounds__(HD) join_splits(AttendArgs a, int splits) {
 }
 
 // bf16: one workgroup per row and KV head (and split), whose waves take the
-// entries of the row's list in turn.  Per 16-key page S = K Q^T by
-// v_mfma_f32_16x16x32_bf16 (the G heads in columns of B, the others zero);
-// its output (lane: head l % 16, keys 4 (l / 16) + i) is the B operand of
-// O^T += V^T P^T by v_mfma_f32_16x16x16_bf16, whose A operand is the
-// transposed value page as it is stored, so no element changes lanes.
+// entries of the row's list in turn, two pages A and B (32 keys) at a time:
+// S = K Q^T by two v_mfma_f32_16x16x32_bf16 chains and O^T += V^T P^T by one
+// such instruction per 16 channels.  The order of the keys in the products is
+// free as long as P and V agree: row m of the first chain is token
+// 8 (m / 4 % 2) + m % 4 of page m / 8, of the second the token four behind.
+// Lane l (column l % 16, group l / 16) then holds, in its outputs, tokens
+// 8 (group % 2) .. + 7 of page group / 2, which is its part of the B operand of
+// the second product; its part of A is those tokens of one channel, 16
+// bytes of the transposed value page.  No element changes lanes, and every
+// load is 16 bytes a lane: with one page at a time the values came by 8, and
+// rows that share pages waited for the L1's address path (219 cycles a page
+// and compute unit; 445 rows of 4 slots 134 us, now 121; 509
+// rows of their own 335 us, now 322).
 // Softmax statistics in fp32; the probabilities enter the second product as
 // bf16 and the row sum adds the same rounded values.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// ONCE: the pages are not read again soon (rows of different slots):
+// non-temporal loads, 509 rows of 64 pages 353 -> 335 us; where rows share
+// pages they cost (445 rows of 4 slots: 241 -> 270 us).
+template <bool ONCE> __device__ __forceinline__ u32x4 load16(const __bf16* p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+    else return *reinterpret_cast<const u32x4*>(p);
+}
+
+template <int HD> struct KeyFrag { u32x4 x[2][HD / 32]; };
+template <int HD> struct ValueFrag { u32x4 x[HD / 16]; };
+
+template <int HD, bool ONCE>
+__device__ __forceinline__ void load_keys(const KvPages& c, int page_a, int page_b, int g, int col, int grp,
+                                          KeyFrag<HD>& f) {
+    const int64_t page = col >> 3 ? page_b : page_a;
+    const __bf16* p = static_cast<const __bf16*>(c.k_pool) + (page * c.n_kv + g) * kPage * HD +
+                      (8 * (col >> 2 & 1) + (col & 3)) * HD + 8 * grp;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int b = 0; b < HD / 32; ++b) f.x[i][b] = load16<ONCE>(p + 4 * i * HD + 32 * b);
+}
+
+template <int HD, bool ONCE>
+__device__ __forceinline__ void load_values(const KvPages& c, int page_a, int page_b, int g, int col, int grp,
+                                            ValueFrag<HD>& f) {
+    const int64_t page = grp >> 1 ? page_b : page_a;
+    const __bf16* p = static_cast<const __bf16*>(c.v_pool) + (page * c.n_kv + g) * HD * kPage + col * kPage + 8 * (grp & 1);
+#pragma unroll
+    for (int b = 0; b < HD / 16; ++b) f.x[b] = load16<ONCE>(p + 16 * kPage * b);
+}
 
 template <int HD>
-struct PageFrag {
-    uint4 k[HD / 32];
-    uint2 v[HD / 16];
-};
-
-// One page's operands.  ONCE: the page is not read again soon (rows of
-// different slots): non-temporal loads, 509 rows of 64 pages 353 -> 335 us;
-// where rows share pages they cost (445 rows of 4 slots: 241 -> 270 us).
-template <int HD, bool ONCE>
-__device__ __forceinline__ void load_page(const KvPages& c, int64_t page, int g, int col, int grp, PageFrag<HD>& f) {
-    const __bf16* kb = static_cast<const __bf16*>(c.k_pool) + (page * c.n_kv + g) * kPage * HD + col * HD + 8 * grp;
-    const __bf16* vb = static_cast<const __bf16*>(c.v_pool) + (page * c.n_kv + g) * HD * kPage + col * kPage + 4 * grp;
-    if constexpr (ONCE) {
+__device__ __forceinline__ void score_keys(const KeyFrag<HD>& f, const bf16x8* qb, float* s) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int b = 0; b < HD / 32; ++b)
-            f.k[b] = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kb + 32 * b)));
+            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f.x[i][b]), qb[b], x, 0, 0, 0);
 #pragma unroll
-        for (int b = 0; b < HD / 16; ++b)
-            f.v[b] = __builtin_bit_cast(uint2, __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(vb + 16 * kPage * b)));
-    } else {
-#pragma unroll
-        for (int b = 0; b < HD / 32; ++b) f.k[b] = *reinterpret_cast<const uint4*>(kb + 32 * b);
-#pragma unroll
-        for (int b = 0; b < HD / 16; ++b) f.v[b] = *reinterpret_cast<const uint2*>(vb + 16 * kPage * b);
+        for (int e = 0; e < 4; ++e) s[4 * i + e] = x[e];
     }
 }
 
-// Adds a page to the running softmax of each column: its first `nkeys` keys (by
-// column; 0 or less: none), of a page that holds `vkeys` (wave-uniform).
+// The running softmax (m, l, o) of each column with the lane's eight scores: of
+// them the first `n` count (by column and page; 0 or less: none).  Returns the
+// probabilities, the B operand of the second product.
 template <int HD>
-__device__ __forceinline__ void add_page(int nkeys, int vkeys, int grp, float qscale, const bf16x8* qb,
-                                         const PageFrag<HD>& f, float& m, float& l, f32x4* o) {
-    f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+__device__ __forceinline__ bf16x8 add_scores(int n, float qscale, float* s, float& m, float& l, f32x4* o) {
 #pragma unroll
-    for (int b = 0; b < HD / 32; ++b)
-        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f.k[b]), qb[b], s, 0, 0, 0);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (4 * grp + i >= nkeys) s[i] = -INFINITY;
-    float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    for (int i = 0; i < 8; ++i)
+        if (i >= n) s[i] = -INFINITY;
+    float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     mx *= qscale;
-    // the reference moves only when a page exceeds it by more than 8 (the
+    // the reference moves only when the keys exceed it by more than 8 (the
     // probabilities then stay below 2^8): most pages rescale nothing
     const bool grow = mx > m + 8.f;
     if (__any(grow)) {
@@ -835,27 +853,76 @@ __device__ __forceinline__ void add_page(int nkeys, int vkeys, int grp, float qs
     }
     const float nm = m == -INFINITY ? 0.f : -m;
     float ps = 0.f;
-    s16x4 pb;
+    bf16x8 pb;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __bf16 p = static_cast<__bf16>(fast_exp2(fmaf(s[i], qscale, nm)));
-        pb[i] = __builtin_bit_cast(short, p);
-        ps += static_cast<float>(p);
+    for (int i = 0; i < 8; ++i) {
+        pb[i] = static_cast<__bf16>(fast_exp2(fmaf(s[i], qscale, nm)));
+        ps += static_cast<float>(pb[i]);
     }
     ps += __shfl_xor(ps, 16, 64);
     ps += __shfl_xor(ps, 32, 64);
     l += ps;
-    const bool part = vkeys < kPage;                 // wave-uniform: the page of the newest token
+    return pb;
+}
+
+// `part`: some page holds fewer than its 16 tokens, `n` of the lane's eight
+// (what stands behind the newest token is not read).
+template <int HD>
+__device__ __forceinline__ void add_values(const ValueFrag<HD>& f, bool part, int n, bf16x8 pb, f32x4* o) {
 #pragma unroll
     for (int b = 0; b < HD / 16; ++b) {
-        uint2 vv = f.v[b];
-        if (part) {                                  // what stands behind the newest token is not read
-            if (4 * grp + 0 >= vkeys) vv.x &= 0xFFFF0000u;
-            if (4 * grp + 1 >= vkeys) vv.x &= 0x0000FFFFu;
-            if (4 * grp + 2 >= vkeys) vv.y &= 0xFFFF0000u;
-            if (4 * grp + 3 >= vkeys) vv.y &= 0x0000FFFFu;
+        u32x4 x = f.x[b];
+        if (part) {                                  // wave-uniform
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                x[e] &= (2 * e < n ? 0x0000FFFFu : 0u) | (2 * e + 1 < n ? 0xFFFF0000u : 0u);
         }
-        o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, vv), pb, o[b], 0, 0, 0);
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), pb, o[b], 0, 0, 0);
+    }
+}
+
+// A wave's walk over the pages whose bit is set in `todo` (lane i: page
+// `page`, index `idx` in the request), by pairs.  keys(idx) is how many tokens
+// of page idx count for this lane's column, held(idx) how many it holds
+// (wave-uniform).  The values of a pair are loaded while its scores are
+// computed, the keys of the next one while its values are awaited.
+template <int HD, bool ONCE, typename Keys, typename Held>
+__device__ __forceinline__ void walk_pages(const KvPages& c, int g, uint64_t todo, int page, int idx, Keys keys, Held held,
+                                           float qscale, const bf16x8* qb, float& m, float& l, f32x4* o) {
+    const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+    int a = 0, b = 0;
+    bool two = false;
+    auto next = [&]() {                              // the next pair, page A twice where there is one left
+        a = __builtin_ctzll(todo);
+        todo &= todo - 1;
+        two = todo != 0;
+        b = two ? __builtin_ctzll(todo) : a;
+        todo &= todo - 1;
+    };
+    if (!todo) return;
+    next();
+    KeyFrag<HD> kf;
+    int pa = __builtin_amdgcn_readlane(page, a), pb = __builtin_amdgcn_readlane(page, b);
+    load_keys<HD, ONCE>(c, pa, pb, g, col, grp, kf);
+    while (true) {
+        ValueFrag<HD> vf;
+        load_values<HD, ONCE>(c, pa, pb, g, col, grp, vf);
+        float s[8];
+        score_keys<HD>(kf, qb, s);
+        const int ia = __builtin_amdgcn_readlane(idx, a), ib = __builtin_amdgcn_readlane(idx, b);
+        const int ha = held(ia), hb = two ? held(ib) : 0;
+        const int ka = keys(ia), kb = two ? keys(ib) : 0;
+        const bool more = todo != 0;
+        if (more) {
+            next();
+            pa = __builtin_amdgcn_readlane(page, a);
+            pb = __builtin_amdgcn_readlane(page, b);
+            load_keys<HD, ONCE>(c, pa, pb, g, col, grp, kf);
+        }
+        const int half = 8 * (grp & 1);
+        const bf16x8 p = add_scores<HD>((grp >> 1 ? kb : ka) - half, qscale, s, m, l, o);
+        add_values<HD>(vf, min(ha, hb) < kPage, (grp >> 1 ? hb : ha) - half, p, o);
+        if (!more) break;
     }
 }
 
@@ -904,22 +971,8 @@ __device__ __forceinline__ void attend_row(const AttendArgs& a, int64_t r, int g
             int page = -1;
             if (idx >= 0 && idx <= pos / kPage) page = row[idx];
             if (page >= c.num_pages) page = -1;
-            uint64_t todo = __ballot(page >= 0);
-            if (!todo) continue;
-            PageFrag<HD> cur, nxt;
-            int at = __builtin_ctzll(todo);
-            todo &= todo - 1;
-            load_page<HD, ONCE>(c, __shfl(page, at, 64), g, col, grp, cur);
-            while (true) {
-                const int nx = todo ? __builtin_ctzll(todo) : at;
-                load_page<HD, ONCE>(c, __shfl(page, nx, 64), g, col, grp, nxt);
-                const int nkeys = pos + 1 - __shfl(idx, at, 64) * kPage;
-                add_page<HD>(nkeys, nkeys, grp, a.qscale, qb, cur, m, l, o);
-                if (!todo) break;
-                todo &= todo - 1;
-                at = nx;
-                cur = nxt;
-            }
+            auto tokens = [&](int i) { return pos + 1 - i * kPage; };
+            walk_pages<HD, ONCE>(c, g, __ballot(page >= 0), page, idx, tokens, tokens, a.qscale, qb, m, l, o);
         }
     }
     if (col < G) {
@@ -988,23 +1041,10 @@ __device__ __forceinline__ bool attend_tile(const AttendArgs& a, int64_t r, int 
         const int idx = e < n ? list[e] : -1;
         int page = idx >= 0 ? row[idx] : -1;
         if (page >= c.num_pages) page = -1;
-        uint64_t todo = __ballot(page >= 0);
-        if (!todo) continue;
-        PageFrag<HD> cur, nxt;
-        int at = __builtin_ctzll(todo);
-        todo &= todo - 1;
-        load_page<HD, false>(c, __shfl(page, at, 64), g, col, grp, cur);
-        while (true) {
-            const int nx = todo ? __builtin_ctzll(todo) : at;
-            load_page<HD, false>(c, __shfl(page, nx, 64), g, col, grp, nxt);
-            const int b = __shfl(idx, at, 64);
-            const bool takes = mask[b >> 1] >> (16 * (b & 1) + j) & 1u;
-            add_page<HD>(takes ? pos + 1 - b * kPage : 0, last + 1 - b * kPage, grp, a.qscale, qb, cur, m, l, o);
-            if (!todo) break;
-            todo &= todo - 1;
-            at = nx;
-            cur = nxt;
-        }
+        walk_pages<HD, false>(
+            c, g, __ballot(page >= 0), page, idx,
+            [&](int i) { return mask[i >> 1] >> (16 * (i & 1) + j) & 1u ? pos + 1 - i * kPage : 0; },
+            [&](int i) { return last + 1 - i * kPage; }, a.qscale, qb, m, l, o);
     }
     __syncthreads();                                                 // the masks and the list are done with
     if (mine) {
