@@ -398,7 +398,8 @@ int64_t outlets_pages_append_workspace(int32_t n_req, int32_t n_rows);
 /*
  * Empties slots (device [n]; -1 is skipped, an empty slot is a no-op) and
  * frees their pages.  status_out [1] (device): 0, or INVALID_ARG with no
- * change for a slot outside [-1, max_slots) or given twice.
+ * change for a slot outside [-1, max_slots) or given twice.  n <= 2^18 (else
+ * UNSUPPORTED).
  */
 int outlets_pages_release(const outlets_page_state* state, int32_t n, const int32_t* slots, int32_t* status_out,
                           void* stream);
@@ -535,8 +536,8 @@ enum {
     OUTLETS_K_FUSE_GEMM = 1,    /* Eq. 1 projection */
     OUTLETS_K_NORM = 2,         /* the RMSNorms (and the embedding gather + norm) */
     OUTLETS_K_QKV_GEMM = 3,
-    OUTLETS_K_ROPE_KV = 4,      /* rotary embedding + paged K/V write */
-    OUTLETS_K_ATTN = 5,
+    OUTLETS_K_ROPE_KV = 4,      /* rotary embedding + paged K/V write; block keys (sparse steps) */
+    OUTLETS_K_ATTN = 5,         /* attention, and the selection of its pages (sparse steps) */
     OUTLETS_K_O_GEMM = 6,
     OUTLETS_K_GATE_UP_GEMM = 7, /* gate/up projection with the SwiGLU epilogue */
     OUTLETS_K_DOWN_GEMM = 8,

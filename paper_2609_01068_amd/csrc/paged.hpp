@@ -22,6 +22,8 @@ struct PageState {
 constexpr int kPageMaxSlots = 1 << 17;
 // Most rows of one append: 1024 requests' sums then fit 31 bits.
 constexpr int kPageMaxRows = 1 << 20;
+// Most slots of one release: each of its blocks looks at all of them.
+constexpr int kReleaseMax = 1 << 18;
 
 void launch_pages_reset(const PageState& s, hipStream_t st);
 // int32 entries of `ws` (0 where the whole call works in LDS).

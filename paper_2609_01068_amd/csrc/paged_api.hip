@@ -166,7 +166,7 @@ int outlets_pages_release(const outlets_page_state* state, int32_t n, const int3
                           void* stream) {
     if (int rc = check_state(state)) return rc;
     if (n < 0) return bad(OUTLETS_ERR_INVALID_ARG, "negative n");
-    if (n > kPageMaxRows) return bad(OUTLETS_ERR_UNSUPPORTED, "more than 2^20 slots");
+    if (n > kReleaseMax) return bad(OUTLETS_ERR_UNSUPPORTED, "more than 2^18 slots");
     if ((n && !slots) || !status_out) return bad(OUTLETS_ERR_INVALID_ARG, "null argument");
     return guarded(state->device, [&] {
         launch_pages_release(state_of(state), n, slots, status_out, static_cast<hipStream_t>(stream));

@@ -717,6 +717,54 @@ def test_attention_of_rows_that_share_a_slot(hd, G, kind):
         assert not bad.any()
 
 
+def test_select_of_denormal_and_huge_values():
+    """Keys below the normal range under large queries: scores of ordinary
+    size, which an instruction that drops denormals would lose."""
+    n_kv, G, hd, top_k = 1, 4, 128, 20
+    table, slots = scattered([1600], 101, 100, 4)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    step = torch.randint(-100, 101, (101, n_kv, hd), generator=g, device="cuda")
+    for fmt, unit, scale in (("bf16", 2.0**-133, 2.0**120), ("f32", 2.0**-149, 2.0**127)):
+        k = (step.double() * unit).to(DT[fmt])
+        q = randn((1, n_kv * G, hd), fmt, 4) * scale
+        kv = cache_over(table, 101, n_kv, hd, fmt, block_keys=k)
+        got = kv.select(q, i32(slots), i32([1599]), top_k, 1, 2).cpu().numpy()
+        want = plain_select(k.double().cpu().numpy(), q.double().cpu().numpy(), table, slots, [1599], n_kv, top_k, 1, 2)
+        assert np.array_equal(got, want), fmt
+
+
+def test_pools_past_32_bit_offsets():
+    """Pages whose elements lie behind 2^31: write, select, attend."""
+    from paper_2609_01068_amd.paged import PagedKV, PageTables
+    n_kv, G, hd, num, top_k = 8, 4, 128, 140000, 9
+    pt = PageTables(num, 3, 700)
+    pt.free_bits.zero_()
+    last = torch.arange(num - 128, num, device="cuda")
+    pt.free_bits[-4:] = -1                              # the pool ends on a whole word
+    kv = PagedKV(pt, n_kv, hd, "bf16")
+    assert kv.k_pool.numel() > 2**31 + 2**27
+    rows = pt.append(i32([2, 0, 1]), i32([640, 333, 700]), 1673)
+    assert rows.status[0].item() == 0 and pt.page_table[2].min().item() == -1
+    k, v = randn((1673, n_kv, hd), "bf16", 1), randn((1673, n_kv, hd), "bf16", 2)
+    kv.write(rows.slot_map, k, v)
+    at = rows.slot_map.long()
+    assert at.min().item() // PAGE >= num - 128
+    assert torch.equal(kv.k_pool[at // PAGE, :, at % PAGE], k) and torch.equal(kv.v_pool[at // PAGE, :, :, at % PAGE], v)
+    # the same on the last pages alone, renumbered
+    table = pt.page_table.cpu().numpy()
+    small = np.where(table >= 0, table - (num - 128), -1)
+    f = lambda t: t[last].double().cpu().numpy()  # noqa: E731
+    rs, pos = np.array([2, 0, 1], dtype=np.int32), np.array([639, 332, 699], dtype=np.int32)
+    q = randn((3, n_kv * G, hd), "bf16", 3)
+    sel = kv.select(q, i32(rs), i32(pos), top_k, 1, 2)
+    want = plain_select(f(kv.block_keys), q.double().cpu().numpy(), small, rs, pos, n_kv, top_k, 1, 2)
+    assert np.array_equal(sel.cpu().numpy(), want)
+    got = kv.attend(q, i32(rs), i32(pos), sel).double().cpu().numpy()
+    ref, e32, e16 = attention_ref(f(kv.k_pool), f(kv.v_pool), q.double().cpu().numpy(), small, rs, pos, want, None)
+    assert (np.abs(got - ref) <= 1.01 * (e32 + e16 + 2.0**-8 * np.abs(ref))).all()
+
+
 # ---------------------------------------------------------------- together
 
 class Serving:

@@ -71,7 +71,7 @@ def test_page_call_refusals():
     refused(r(C.byref(s), -1, A, A, None), INV)
     refused(r(C.byref(s), 1, None, A, None), INV)
     refused(r(C.byref(s), 1, A, None, None), INV)
-    refused(r(C.byref(s), (1 << 20) + 1, A, A, None), UNS)
+    refused(r(C.byref(s), (1 << 18) + 1, A, A, None), UNS)
 
 
 def write(c, n=1, sm=A, k=A, ks=256, v=A, vs=256):
