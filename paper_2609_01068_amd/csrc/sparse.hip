@@ -15,6 +15,20 @@ __device__ __forceinline__ double to_f64(__bf16 x) { return static_cast<double>(
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__bf16 x) { return static_cast<float>(x); }
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Byte address for ds_bpermute: from lanes by rows of four to a product's
+// order, row l % 16 and 16 bytes l / 16.
+__device__ __forceinline__ int product_lane() {
+    return 4 * (4 * (threadIdx.x & 15) + (threadIdx.x >> 4 & 3));
+}
+__device__ __forceinline__ u32x4 to_product(u32x4 x, int from) {
+    u32x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = __builtin_amdgcn_ds_bpermute(from, x[e]);
+    return y;
+}
+
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // ---------------------------------------------------------------- scores
@@ -121,17 +135,18 @@ __device__ __forceinline__ uint32_t score_pages_bf16(const SelectArgs& a, int r,
         hi[i] = nb > a.top_k ? nb - a.local : 0;
     }
     uint32_t big = 0;
+    const int from = product_lane();
     for (int p = p0; p < p1; p += step) {
         int id = next;
         next = ids(p + step);
         if (id >= a.c.num_pages) id = -1;
-        uint4 kf[4][HD / 32];
+        u32x4 kf[4][HD / 32];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int64_t page = max(__shfl(id, 16 * u + col, 64), 0);
-            const __bf16* src = keys + (page * a.c.n_kv + g) * HD + 8 * grp;
+            const int64_t page = max(__shfl(id, 16 * u + (lane >> 2), 64), 0);
+            const __bf16* src = keys + (page * a.c.n_kv + g) * HD + 8 * (lane & 3);
 #pragma unroll
-            for (int b = 0; b < HD / 32; ++b) kf[u][b] = *reinterpret_cast<const uint4*>(src + 32 * b);
+            for (int b = 0; b < HD / 32; ++b) kf[u][b] = *reinterpret_cast<const u32x4*>(src + 32 * b);
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -139,9 +154,9 @@ __device__ __forceinline__ uint32_t score_pages_bf16(const SelectArgs& a, int r,
             f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f}, m = s;
 #pragma unroll
             for (int b = 0; b < HD / 32; ++b) {
-                uint4 x = kf[u][b];
+                u32x4 x = to_product(kf[u][b], from);
                 s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[b], __builtin_bit_cast(bf16x8, x), s, 0, 0, 0);
-                x.x &= 0x7FFF7FFFu; x.y &= 0x7FFF7FFFu; x.z &= 0x7FFF7FFFu; x.w &= 0x7FFF7FFFu;
+                x &= 0x7FFF7FFFu;
                 m = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qm[b], __builtin_bit_cast(bf16x8, x), m, 0, 0, 0);
             }
             const int b = p + 16 * u + col;
@@ -781,8 +796,6 @@ __global__ void __launch_bounds__(HD) join_splits(AttendArgs a, int splits) {
 // rows of their own 335 us, now 322).
 // Softmax statistics in fp32; the probabilities enter the second product as
 // bf16 and the row sum adds the same rounded values.
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 // ONCE: the pages are not read again soon (rows of different slots):
 // non-temporal loads, 509 rows of 64 pages 353 -> 335 us; where rows share
 // pages they cost (445 rows of 4 slots: 241 -> 270 us).
@@ -794,12 +807,18 @@ template <bool ONCE> __device__ __forceinline__ u32x4 load16(const __bf16* p) {
 template <int HD> struct KeyFrag { u32x4 x[2][HD / 32]; };
 template <int HD> struct ValueFrag { u32x4 x[HD / 16]; };
 
+// The keys of a pair.  ONCE: as the product takes them, lane l row l % 16 and
+// 16 bytes l / 16.  Otherwise lane l holds 16 bytes l % 4 of row l / 4, and
+// score_keys exchanges lanes: four neighbouring lanes then read 64
+// neighbouring bytes, and a load takes the L1 17 cycles instead of 64 (445 rows
+// of 4 slots 121 -> 99 us; 509 rows of their own wait for memory, 322 us
+// without the exchange and 329 us with it).
 template <int HD, bool ONCE>
-__device__ __forceinline__ void load_keys(const KvPages& c, int page_a, int page_b, int g, int col, int grp,
-                                          KeyFrag<HD>& f) {
-    const int64_t page = col >> 3 ? page_b : page_a;
+__device__ __forceinline__ void load_keys(const KvPages& c, int page_a, int page_b, int g, int lane, KeyFrag<HD>& f) {
+    const int m = ONCE ? lane & 15 : lane >> 2, chunk = ONCE ? lane >> 4 : lane & 3;
+    const int64_t page = m >> 3 ? page_b : page_a;
     const __bf16* p = static_cast<const __bf16*>(c.k_pool) + (page * c.n_kv + g) * kPage * HD +
-                      (8 * (col >> 2 & 1) + (col & 3)) * HD + 8 * grp;
+                      (8 * (m >> 2 & 1) + (m & 3)) * HD + 8 * chunk;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -815,14 +834,17 @@ __device__ __forceinline__ void load_values(const KvPages& c, int page_a, int pa
     for (int b = 0; b < HD / 16; ++b) f.x[b] = load16<ONCE>(p + 16 * kPage * b);
 }
 
-template <int HD>
+template <int HD, bool ONCE>
 __device__ __forceinline__ void score_keys(const KeyFrag<HD>& f, const bf16x8* qb, float* s) {
+    const int from = product_lane();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int b = 0; b < HD / 32; ++b)
-            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f.x[i][b]), qb[b], x, 0, 0, 0);
+        for (int b = 0; b < HD / 32; ++b) {
+            const u32x4 k = ONCE ? f.x[i][b] : to_product(f.x[i][b], from);
+            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), qb[b], x, 0, 0, 0);
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[4 * i + e] = x[e];
     }
@@ -903,12 +925,12 @@ __device__ __forceinline__ void walk_pages(const KvPages& c, int g, uint64_t tod
     next();
     KeyFrag<HD> kf;
     int pa = __builtin_amdgcn_readlane(page, a), pb = __builtin_amdgcn_readlane(page, b);
-    load_keys<HD, ONCE>(c, pa, pb, g, col, grp, kf);
+    load_keys<HD, ONCE>(c, pa, pb, g, lane, kf);
     while (true) {
         ValueFrag<HD> vf;
         load_values<HD, ONCE>(c, pa, pb, g, col, grp, vf);
         float s[8];
-        score_keys<HD>(kf, qb, s);
+        score_keys<HD, ONCE>(kf, qb, s);
         const int ia = __builtin_amdgcn_readlane(idx, a), ib = __builtin_amdgcn_readlane(idx, b);
         const int ha = held(ia), hb = two ? held(ib) : 0;
         const int ka = keys(ia), kb = two ? keys(ib) : 0;
@@ -917,7 +939,7 @@ __device__ __forceinline__ void walk_pages(const KvPages& c, int g, uint64_t tod
             next();
             pa = __builtin_amdgcn_readlane(page, a);
             pb = __builtin_amdgcn_readlane(page, b);
-            load_keys<HD, ONCE>(c, pa, pb, g, col, grp, kf);
+            load_keys<HD, ONCE>(c, pa, pb, g, lane, kf);
         }
         const int half = 8 * (grp & 1);
         const bf16x8 p = add_scores<HD>((grp >> 1 ? kb : ka) - half, qscale, s, m, l, o);
