@@ -55,8 +55,9 @@ struct SelectArgs {
     int64_t ldq;
     int n_rows, G, top_k, sink, local;
     int tile;              // rows scored together where they belong to one slot
-    uint64_t* keys;        // [rows, n_kv, max_pages]: 64-bit scores of crowded borders
-    float* scores;         // [rows, n_kv, max_pages] (split form)
+    int ld;                // scores of a row: max_pages, to a multiple of kPad
+    uint64_t* keys;        // [rows, n_kv, ld]: 64-bit scores of crowded borders
+    float* scores;         // [rows, n_kv, ld] (split form)
     float* bounds;         // [rows, n_kv, chunks] (split form)
     int32_t* sel;
 };
@@ -375,6 +376,9 @@ __device__ __forceinline__ double exact_score(const KvPages& c, const T* q, int 
     return s;
 }
 
+// Scores that a wave takes at a time; rows of scores are padded to it.
+constexpr int kPad = 256;
+
 // The scores of a row, dealt to the waves of a group in contiguous parts.
 // Loops over them stay loops: a selection is a dozen short passes, and
 // unrolled over scores held in registers their code did not fit the
@@ -382,21 +386,20 @@ __device__ __forceinline__ double exact_score(const KvPages& c, const T* q, int 
 template <int NT>
 struct RowScores {
     float* sc;
-    int first, end;            // the wave's pages
+    int first, end;            // the wave's pages, the last ones behind the row's
 
     __device__ __forceinline__ RowScores(float* scores, int nb) : sc(scores) {
-        const int part = (nb + NT - 1) / NT * 64;
+        const int part = (nb + NT * 4 - 1) / (NT * 4) * kPad, padded = (nb + kPad - 1) / kPad * kPad;
         first = (threadIdx.x % NT >> 6) * part;
-        end = min(first + part, nb);
+        end = min(first + part, padded);
     }
-    // f(page, score) for every page of the wave's part and some behind it, all
-    // lanes together; U scores in flight (1 where the pass is rare)
+    // f(page, score) for every page of the wave's part, all lanes together; U
+    // scores in flight (1 where the pass is rare)
     template <int U = 4, typename F> __device__ __forceinline__ void each(F f) const {
-        const int lane = threadIdx.x & 63;
-        for (int i = first + lane; i - lane < end; i += 64 * U) {
+        for (int i = first + static_cast<int>(threadIdx.x & 63); i < end; i += 64 * U) {
             float v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = sc[min(i + 64 * u, end - 1)];
+            for (int u = 0; u < U; ++u) v[u] = sc[i + 64 * u];
 #pragma unroll
             for (int u = 0; u < U; ++u) f(i + 64 * u, v[u]);
         }
@@ -414,7 +417,12 @@ __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, f
     const int lo = a.sink, hi = nb - a.local, want = a.top_k - a.sink - a.local;
     int32_t* sel = a.sel + (static_cast<int64_t>(r) * a.c.n_kv + g) * a.top_k;
     const RowScores<NT> row(sc, nb);
-    auto among = [&](int i) { return i >= lo && i < hi && i < row.end; };
+    auto among = [&](int i) { return i >= lo && i < hi; };
+    // NaN outside the candidates: no comparison takes them in, and the passes
+    // need no other test (half their instructions were such tests)
+    for (int i = tid; i < lo; i += NT) sc[i] = __builtin_nanf("");
+    for (int i = hi + tid; i < (nb + kPad - 1) / kPad * kPad; i += NT) sc[i] = __builtin_nanf("");
+    group_sync<NT>();
     const float d2 = bound * kScoreErr2 + kScoreErrAbs;
     float thr = INFINITY;                            // pages of at least this score are taken
     if (want > 0) {
@@ -425,10 +433,9 @@ __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, f
             // the want-th largest score t, to one of 256 bins between the
             // extremes (of a linear scale: its bins hold few pages each)
             float mn = INFINITY, mx = -INFINITY;
-            row.each([&](int i, float s) {
-                if (!among(i)) return;
+            row.each([&](int, float s) {
                 mx = fmaxf(mx, s);
-                if (s > -INFINITY) mn = fminf(mn, s);
+                mn = fminf(mn, s == -INFINITY ? INFINITY : s);
             });
 #pragma unroll
             for (int o = 32; o > 0; o >>= 1) {
@@ -445,8 +452,8 @@ __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, f
             auto bin = [&](float s) {                // nondecreasing in s
                 return s > mn ? min(static_cast<int>((s - mn) * scale), 255) : 0;
             };
-            row.each([&](int i, float s) {
-                if (among(i)) atomicAdd(&sh.hist[bin(s)], 1);
+            row.each([&](int, float s) {
+                if (s == s) atomicAdd(&sh.hist[bin(s)], 1);
             });
             group_sync<NT>();
             find_bin<NT>(want, sh);
@@ -457,11 +464,10 @@ __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, f
             const float B = static_cast<float>(sh.bin), width = (mx - mn) / 255.f;
             upper = mn + (B + 1.01f) * width + d2;
             lower = sh.bin == 0 ? -INFINITY : mn + (B - 0.01f) * width - d2;
-            int in = 0, crowded = 0;
+            int in = 0;
             row.each([&](int i, float s) {
-                const bool is_in = among(i) && s > upper, close = among(i) && s >= lower && !is_in;
-                in += is_in;
-                if (close) {
+                in += s > upper;
+                if (s >= lower && !(s > upper)) {
                     const int k = atomicAdd(&sh.n, 1);
                     if (k < kNear) sh.index[k] = i;
                 }
@@ -547,21 +553,24 @@ __device__ void pick_row(const SelectArgs& a, int r, int g, int nb, float* sc, f
             }
         }
     }
+    if (want == 0) row.template each<1>([&](int i, float) { sc[i] = __builtin_nanf(""); });
+    group_sync<NT>();
+    for (int i = tid; i < lo; i += NT) sc[i] = INFINITY;
+    for (int i = hi + tid; i < nb; i += NT) sc[i] = INFINITY;
+    group_sync<NT>();
     // each wave lists its part, behind those of the waves before it
-    auto takes = [&](int i, float s) { return i < row.end && (i < lo || i >= hi || (want > 0 && s >= thr)); };
     int at = 0;
     if (NW > 1) {
         int n = 0;
-        row.each([&](int i, float s) { n += __popcll(__ballot(takes(i, s))); });
+        row.each([&](int, float s) { n += __popcll(__ballot(s >= thr)); });
         if (lane == 0) sh.red[w] = n;
         group_sync<NT>();
 #pragma unroll
         for (int j = 0; j < NW; ++j) at += j < w ? sh.red[j] : 0;
     }
     row.each([&](int i, float s) {
-        const bool take = takes(i, s);
-        const uint64_t m = __ballot(take);
-        if (take) sel[at + __popcll(m & ((1ull << lane) - 1))] = i;
+        const uint64_t m = __ballot(s >= thr);
+        if (s >= thr) sel[at + __builtin_amdgcn_mbcnt_hi(m >> 32, __builtin_amdgcn_mbcnt_lo(m, 0))] = i;
         at += __popcll(m);
     });
     group_sync<NT>();
@@ -590,10 +599,10 @@ constexpr int kUnit = 64;            // pages that a wave scores at a time
 template <typename T, int HD, int GP, int NW>
 __global__ void __launch_bounds__(64 * NW)
 block_select_fused(SelectArgs a) {
-    extern __shared__ float sc[];                    // [tile][max_pages]
+    extern __shared__ float sc[];                    // [tile][ld]
     __shared__ PickShared<64> sh[NW];
     __shared__ uint32_t bound;
-    const int w = threadIdx.x >> 6, ld = a.c.max_pages;
+    const int w = threadIdx.x >> 6, ld = a.ld;
     const int x = blockIdx.x % 8, y = blockIdx.x / 8, g = y % a.c.n_kv;
     const int r = (y / a.c.n_kv * 8 + x) * a.tile + blockIdx.y;
     if (r >= a.n_rows) return;
@@ -636,8 +645,8 @@ block_scores(SelectArgs a) {
     for (int j = 0; j < nr; ++j) most = max(most, visible_pages(a, r + j));
     if (most <= a.top_k) return;
     uint32_t big = score_pages<T, HD, GP>(a, r, nr, g, blockIdx.x * kUnit, kUnit, slices * kUnit, most - a.local,
-                                          a.scores + (static_cast<int64_t>(r) * a.c.n_kv + g) * a.c.max_pages,
-                                          static_cast<int64_t>(a.c.n_kv) * a.c.max_pages);
+                                          a.scores + (static_cast<int64_t>(r) * a.c.n_kv + g) * a.ld,
+                                          static_cast<int64_t>(a.c.n_kv) * a.ld);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) big = max(big, __shfl_xor(big, o, 64));
     if (threadIdx.x < nr)
@@ -647,7 +656,7 @@ block_scores(SelectArgs a) {
 template <typename T, int HD, int NT, bool LDS>
 __global__ void __launch_bounds__(NT)
 block_pick(SelectArgs a, int slices) {
-    extern __shared__ float lds[];                   // [max_pages]
+    extern __shared__ float lds[];                   // [ld]
     __shared__ PickShared<NT> sh;
     __shared__ uint32_t bound;
     const int g = blockIdx.x, r = blockIdx.y, nb = visible_pages(a, r);
@@ -656,7 +665,7 @@ block_pick(SelectArgs a, int slices) {
         return;
     }
     const int64_t item = static_cast<int64_t>(r) * a.c.n_kv + g;
-    float* sc = a.scores + item * a.c.max_pages;
+    float* sc = a.scores + item * a.ld;
     if (threadIdx.x == 0) bound = 0;
     __syncthreads();
     if (LDS) {
@@ -675,7 +684,7 @@ block_pick(SelectArgs a, int slices) {
         if (b) atomicMax(&bound, b);
     }
     __syncthreads();
-    uint64_t* keys = a.keys + item * a.c.max_pages;
+    uint64_t* keys = a.keys + item * a.ld;
     if constexpr (LDS) pick_row<T, HD, NT>(a, r, g, nb, lds, __uint_as_float(bound), keys, sh);
     else pick_row<T, HD, NT>(a, r, g, nb, sc, __uint_as_float(bound), keys, sh);
 }
@@ -1203,9 +1212,11 @@ block_attend_f32(AttendArgs a) {
 // where the table is that long.
 static int score_slices(const KvPages& c) { return 8 * std::max(1, (c.max_pages + kUnit - 1) / kUnit / 24); }
 
+static int score_stride(const KvPages& c) { return (c.max_pages + kPad - 1) / kPad * kPad; }
+
 int64_t block_select_ws(const KvPages& c, int64_t n_rows) {
     // 64-bit keys, 32-bit scores, bounds
-    const int64_t row = c.n_kv * (static_cast<int64_t>(c.max_pages) * 12 + 4 * score_slices(c));
+    const int64_t row = c.n_kv * (static_cast<int64_t>(score_stride(c)) * 12 + 4 * score_slices(c));
     return n_rows * ((row + 15) / 16 * 16);
 }
 
@@ -1218,6 +1229,7 @@ void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int
     // every row sees all it may read: no scores, no workspace
     const bool plain = c.max_pages <= top_k;
     const bool fused = plain || c.max_pages <= kFusedPages;
+    const int ld = score_stride(c);
     const int slab = static_cast<int>(std::min<int64_t>(plain ? rows.n_rows : ws_bytes / row_bytes,
                                                         std::min(rows.n_rows, 32768)));     // (the grid's z)
     // Enough rows to fill the chip with a wave each, and not so many that slots
@@ -1225,20 +1237,20 @@ void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int
     const bool alone = fused && rows.n_rows < 2 * c.max_slots && static_cast<int64_t>(rows.n_rows) * c.n_kv >= 8 * cus;
     int tile = plain || alone ? 1 : 16 / gp;
     if (fused)
-        while (tile > 1 && tile * c.max_pages * 4 > kFusedBytes) tile /= 2;
+        while (tile > 1 && tile * ld * 4 > kFusedBytes) tile /= 2;
     for (int r0 = 0; r0 < rows.n_rows; r0 += slab) {
         const int n = std::min(slab, rows.n_rows - r0);
         const int64_t items = static_cast<int64_t>(n) * c.n_kv;
         uint64_t* keys = static_cast<uint64_t*>(ws);
-        float* scores = plain ? nullptr : reinterpret_cast<float*>(keys + items * c.max_pages);
+        float* scores = plain ? nullptr : reinterpret_cast<float*>(keys + items * ld);
         const SelectArgs a{c,     rows.row_slot + r0, rows.positions + r0,
                            static_cast<const char*>(rows.q) + eb * rows.ldq * r0,
-                           rows.ldq, n, G, top_k, sink, local, tile, keys, scores,
-                           plain ? nullptr : scores + items * c.max_pages, sel + static_cast<int64_t>(r0) * c.n_kv * top_k};
+                           rows.ldq, n, G, top_k, sink, local, tile, ld, keys, scores,
+                           plain ? nullptr : scores + items * ld, sel + static_cast<int64_t>(r0) * c.n_kv * top_k};
 #define OUTLETS_SELECT(T, HD, GP)                                                                                 \
     do {                                                                                                          \
         const dim3 blocks((n + 8 * tile - 1) / (8 * tile) * 8 * c.n_kv, tile);                                    \
-        const size_t lds = plain ? 0 : sizeof(float) * tile * c.max_pages;                                        \
+        const size_t lds = plain ? 0 : sizeof(float) * tile * ld;                                        \
         if (alone) {                                                                                              \
             hipLaunchKernelGGL((block_select_fused<T, HD, GP, 1>), blocks, dim3(64), lds, st, a);                   \
         } else if (fused) {                                                                                       \
@@ -1252,8 +1264,8 @@ void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int
     } while (0)
 #define OUTLETS_PICK(T, HD, NT)                                                                                   \
     do {                                                                                                          \
-        if (c.max_pages <= kPickLdsPages)                                                                         \
-            hipLaunchKernelGGL((block_pick<T, HD, NT, true>), dim3(c.n_kv, n), dim3(NT), sizeof(float) * c.max_pages, st, \
+        if (ld <= kPickLdsPages)                                                                         \
+            hipLaunchKernelGGL((block_pick<T, HD, NT, true>), dim3(c.n_kv, n), dim3(NT), sizeof(float) * ld, st, \
                                a, slices);                                                                        \
         else                                                                                                      \
             hipLaunchKernelGGL((block_pick<T, HD, NT, false>), dim3(c.n_kv, n), dim3(NT), 0, st, a, slices);          \
