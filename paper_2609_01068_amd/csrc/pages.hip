@@ -287,12 +287,12 @@ template <typename T> __device__ __forceinline__ T block_mean(double sum) {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// Calls of this many rows on: tiles of 32 rows (fewer rows are looked at
-// twice; small calls need the workgroups of 16) and non-temporal stores, for
-// what a call of 32 MB or more leaves in no cache (37,800 rows of 8 heads,
-// 310 MB read and written: 88 us with tiles of 16 rows, 80 with 32, 66 with
-// such stores; a copy of as many bytes takes 61).
-constexpr int kBigWrite = 8192;
+// Calls of this many rows on take tiles of 32 rows, which look at fewer rows
+// twice, and non-temporal stores (37,800 rows of 8 heads, 310 MB read and
+// written: 88 us with tiles of 16 rows, 80 with 32, 66 with such stores; a copy
+// of as many bytes takes 61; 4,000 rows 12.2 and 10.8 us, 1,000 rows 9.0 and
+// 8.9); single rows need the workgroups of 16 (509 of them: 8.7 and 11.9).
+constexpr int kBigWrite = 2048;
 
 template <bool STREAM> __device__ __forceinline__ void put16(void* p, u32x4 x) {
     if constexpr (STREAM) __builtin_nontemporal_store(x, static_cast<u32x4*>(p));

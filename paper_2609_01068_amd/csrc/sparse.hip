@@ -583,7 +583,9 @@ __device__ __forceinline__ void pick_all(const SelectArgs& a, int r, int g, int 
     for (int i = threadIdx.x % NT; i < a.top_k; i += NT) sel[i] = i < nb ? i : -1;
 }
 
-constexpr int kFusedPages = 1024;    // tables up to this many pages take the fused form
+// Tables up to this many pages take the fused form (512 rows of 268 pages on
+// average: 55 us, 86 split; 64 rows of 750: 30 and 32; 8 rows: 19 and 15).
+constexpr int kFusedPages = 1024;
 constexpr int kPickLdsPages = 12288; // scores of a row that the split form copies to LDS (48 KB)
 constexpr int kUnit = 64;            // pages that a wave scores at a time
 
@@ -593,12 +595,14 @@ constexpr int kUnit = 64;            // pages that a wave scores at a time
 // head (416 prompt rows of 1,650 pages, scores alone: 192 us by head, 75 us
 // by row).
 //
-// Fused form: one block of NW waves per KV head and row (or tile of rows),
+// Fused form: one block of four waves per KV head and row (or tile of rows),
 // blocks i and i + 8, which share an XCD, taking the heads of one tile.
-// Scores in LDS by all waves, then a wave per row selects.
-template <typename T, int HD, int GP, int NW>
-__global__ void __launch_bounds__(64 * NW)
+// Scores in LDS by all waves, then a wave per row selects (a wave per block,
+// which waits for no other: 57 us against 55 for 512 rows).
+template <typename T, int HD, int GP>
+__global__ void __launch_bounds__(256)
 block_select_fused(SelectArgs a) {
+    constexpr int NW = 4;
     extern __shared__ float sc[];                    // [tile][ld]
     __shared__ PickShared<64> sh[NW];
     __shared__ uint32_t bound;
@@ -612,13 +616,13 @@ block_select_fused(SelectArgs a) {
     for (int j = 0; j < nr; ++j) most = max(most, visible_pages(a, r + j));
     if (most > a.top_k) {                            // uniform over the block
         if (threadIdx.x == 0) bound = 0;
-        group_sync<64 * NW>();
+        __syncthreads();
         // equal shares of 16 pages; a wave's part begins where the last one's ends
         const int first = a.sink, end = most - a.local, tiles = (end - first + 15) / 16;
         const uint32_t big = score_pages<T, HD, GP>(a, r, nr, g, first + 16 * (tiles * w / NW), kUnit, kUnit,
                                                     min(first + 16 * (tiles * (w + 1) / NW), end), sc, ld);
         if (big) atomicMax(&bound, big);
-        group_sync<64 * NW>();
+        __syncthreads();
     }
     for (int j = w; j < nr; j += NW) {
         const int nb = visible_pages(a, r + j);
@@ -631,10 +635,11 @@ block_select_fused(SelectArgs a) {
 
 // Split form, for long tables: units of 64 pages dealt to gridDim.x waves (a
 // multiple of 8), so that an XCD scores the same pages for all rows and heads
-// and finds their block keys in its L2; then one block per row and KV head
-// selects: of 1,024 threads where there are fewer blocks than compute units
-// (48 of 3,750 to 8,192 pages: 18 us against 33 us with 256), else of 256
-// (3,328 of 1,650 pages: 35 us against 122 us).
+// and finds their block keys in its L2; then one group of threads per row and
+// KV head selects: 1,024 where there are fewer groups than compute units (48
+// of 3,750 to 8,192 pages: 14 us, 19 with 256, 46 with 64), 64 where there are
+// four a compute unit (3,328 of 1,650 pages: 24 us, 34 with 256, 110 with
+// 1,024), 256 between.
 template <typename T, int HD, int GP>
 __global__ void __launch_bounds__(64)
 block_scores(SelectArgs a) {
@@ -1232,10 +1237,7 @@ void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int
     const int ld = score_stride(c);
     const int slab = static_cast<int>(std::min<int64_t>(plain ? rows.n_rows : ws_bytes / row_bytes,
                                                         std::min(rows.n_rows, 32768)));     // (the grid's z)
-    // Enough rows to fill the chip with a wave each, and not so many that slots
-    // must have several of them: one wave per block, none of which waits.
-    const bool alone = fused && rows.n_rows < 2 * c.max_slots && static_cast<int64_t>(rows.n_rows) * c.n_kv >= 8 * cus;
-    int tile = plain || alone ? 1 : 16 / gp;
+    int tile = plain ? 1 : 16 / gp;
     if (fused)
         while (tile > 1 && tile * ld * 4 > kFusedBytes) tile /= 2;
     for (int r0 = 0; r0 < rows.n_rows; r0 += slab) {
@@ -1251,10 +1253,8 @@ void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int
     do {                                                                                                          \
         const dim3 blocks((n + 8 * tile - 1) / (8 * tile) * 8 * c.n_kv, tile);                                    \
         const size_t lds = plain ? 0 : sizeof(float) * tile * ld;                                        \
-        if (alone) {                                                                                              \
-            hipLaunchKernelGGL((block_select_fused<T, HD, GP, 1>), blocks, dim3(64), lds, st, a);                   \
-        } else if (fused) {                                                                                       \
-            hipLaunchKernelGGL((block_select_fused<T, HD, GP, 4>), blocks, dim3(256), lds, st, a);                  \
+        if (fused) {                                                                                              \
+            hipLaunchKernelGGL((block_select_fused<T, HD, GP>), blocks, dim3(256), lds, st, a);                     \
         } else {                                                                                                  \
             hipLaunchKernelGGL((block_scores<T, HD, GP>), dim3(slices, c.n_kv, n), dim3(64), 0, st, a); \
             if (items < cus) OUTLETS_PICK(T, HD, 1024);                                                            \
