@@ -382,7 +382,7 @@ constexpr int kPad = 256;
 // The scores of a row, dealt to the waves of a group in contiguous parts.
 // Loops over them stay loops: a selection is a dozen short passes, and
 // unrolled over scores held in registers their code did not fit the
-// instruction cache (3,328 selections of 1,650 pages 35 -> 71 us).
+// instruction cache (3,560 selections of 1,650 pages 35 -> 71 us).
 template <int NT>
 struct RowScores {
     float* sc;
@@ -583,7 +583,7 @@ __device__ __forceinline__ void pick_all(const SelectArgs& a, int r, int g, int 
     for (int i = threadIdx.x % NT; i < a.top_k; i += NT) sel[i] = i < nb ? i : -1;
 }
 
-// Tables up to this many pages take the fused form (512 rows of 268 pages on
+// Tables up to this many pages take the fused form (512 rows of 264 pages on
 // average: 55 us, 86 split; 64 rows of 750: 30 and 32; 8 rows: 19 and 15).
 constexpr int kFusedPages = 1024;
 constexpr int kPickLdsPages = 12288; // scores of a row that the split form copies to LDS (48 KB)
@@ -592,7 +592,7 @@ constexpr int kUnit = 64;            // pages that a wave scores at a time
 // A KV head's part of a block key (256 bytes at 128 channels) falls on few of
 // an L2's channels, the same for every page, so an XCD that worked on one
 // head would use a fraction of its L2: the grids below give each XCD every
-// head (416 prompt rows of 1,650 pages, scores alone: 192 us by head, 75 us
+// head (445 prompt rows of 1,650 pages, scores alone: 192 us by head, 75 us
 // by row).
 //
 // Fused form: one block of four waves per KV head and row (or tile of rows),
@@ -638,7 +638,7 @@ block_select_fused(SelectArgs a) {
 // and finds their block keys in its L2; then one group of threads per row and
 // KV head selects: 1,024 where there are fewer groups than compute units (48
 // of 3,750 to 8,192 pages: 14 us, 19 with 256, 46 with 64), 64 where there are
-// four a compute unit (3,328 of 1,650 pages: 24 us, 34 with 256, 110 with
+// four a compute unit (3,560 of 1,650 pages: 24 us, 34 with 256, 110 with
 // 1,024), 256 between.
 template <typename T, int HD, int GP>
 __global__ void __launch_bounds__(64)
