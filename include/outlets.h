@@ -472,7 +472,7 @@ int64_t outlets_block_select_workspace(const outlets_kv_pages* cache, int32_t n_
  *   q as above, rows 16-byte aligned (else UNSUPPORTED).
  *   gate (nullable): laid out like q with its own stride; output element x is
  *     multiplied by sigmoid(gate x) (the attention output gate).
- *   out: fmt, row r at element r * out_stride.
+ *   out: fmt, row r at element r * out_stride; must not overlap q or gate.
  *   ws: outlets_block_attention_workspace(...) bytes (may be 0), 16-byte aligned.
  */
 int outlets_block_attention(const outlets_kv_pages* cache, int32_t n_rows, const int32_t* row_slot,

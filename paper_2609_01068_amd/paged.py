@@ -220,7 +220,8 @@ class PagedKV:
     @_on_stream
     def attend(self, q: torch.Tensor, row_slot: torch.Tensor, positions: torch.Tensor, sel: torch.Tensor,
                gate: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """Attention [n, n_q, hd] of each row over the pages of ``sel`` (as ``select`` gives them)."""
+        """Attention [n, n_q, hd] of each row over the pages of ``sel`` (as
+        ``select`` gives them); ``out`` must not overlap ``q`` or ``gate``."""
         n, n_q = q.shape[0], q.shape[1]
         lib, index = B.lib(), self._index
         qp, qs = self._heads(q, "q", n, n_q)

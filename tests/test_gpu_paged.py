@@ -202,6 +202,19 @@ def test_pools_larger_than_the_kept_words():
     assert sorted(free_pages(pt)) == free[n:]
 
 
+def test_most_slots():
+    """The largest slot count, at both ends of its range."""
+    n = 1 << 17
+    pt = tables(40, n, 32)
+    rows = pt.append(i32([n - 1, 0, n - 2]), i32([17, 3, 32]), 60)
+    assert rows.status.tolist() == [0, 52, 5, 35]
+    check_rows(pt, rows, [n - 1, 0, n - 2], [17, 3, 32], np.zeros(n, dtype=int), 60)
+    assert pt.append(i32([0, n - 1, 0]), i32([1, 1, 1]), 60).status[0].item() == B.OUTLETS_ERR_INVALID_ARG
+    assert pt.release(i32([n - 1, n])).item() == B.OUTLETS_ERR_INVALID_ARG
+    assert pt.append(i32([-1] * 5000 + [n - 1]), i32([1] * 5001), 5000).status.tolist() == [0, 1, 0, 35]
+    assert pt.release(i32([n - 1, -1, 0])).item() == 0 and len(free_pages(pt)) == 38
+
+
 # ---------------------------------------------------------------- cache write
 
 def make_kv(pt, n_kv, hd, fmt, seed=0, scale=1.0):
@@ -764,6 +777,29 @@ def test_pools_past_32_bit_offsets():
     got = kv.attend(q, i32(rs), i32(pos), sel).double().cpu().numpy()
     ref, e32, e16 = attention_ref(f(kv.k_pool), f(kv.v_pool), q.double().cpu().numpy(), small, rs, pos, want, None)
     assert (np.abs(got - ref) <= 1.01 * (e32 + e16 + 2.0**-8 * np.abs(ref))).all()
+
+
+@pytest.mark.parametrize("fmt", ["f32", "bf16"])
+def test_more_rows_than_one_launch(fmt):
+    """Rows past a grid's limit, of slots that change every row and of one slot."""
+    n, n_kv, G, hd, top_k, slots = 70001, 1, 2, 64, 2, 7
+    table = np.arange(slots * 4, dtype=np.int32).reshape(slots, 4)
+    r = np.random.default_rng(0)
+    row_slot = np.where(np.arange(n) < 40000, np.arange(n) % slots, 3).astype(np.int32)
+    pos = r.integers(0, 64, size=n).astype(np.int32)
+    k, v = randn((28, n_kv, PAGE, hd), fmt, 1), randn((28, n_kv, hd, PAGE), fmt, 2)
+    keys = (k.double().mean(dim=2)).to(DT[fmt])
+    kv = cache_over(table, 28, n_kv, hd, fmt, k_pool=k, v_pool=v, block_keys=keys)
+    q = randn((n, n_kv * G, hd), fmt, 3)
+    sel = kv.select(q, i32(row_slot), i32(pos), top_k, 0, 1)
+    got = kv.attend(q, i32(row_slot), i32(pos), sel)
+    rows = np.unique(np.concatenate([r.integers(0, n, size=300), [0, 32767, 32768, 32769, 39999, 40000, 65535, 65536, n - 1]]))
+    f = lambda t: t.double().cpu().numpy()  # noqa: E731
+    want = plain_select(f(keys), f(q[rows]), table, row_slot[rows], pos[rows], n_kv, top_k, 0, 1)
+    assert np.array_equal(sel[rows].cpu().numpy(), want)
+    ref, e32, e16 = attention_ref(f(k), f(v), f(q[rows]), table, row_slot[rows], pos[rows], want, None)
+    tol = 1.01 * (e32 + (e16 + 2.0**-8 * np.abs(ref) if fmt == "bf16" else 2.0**-24 * np.abs(ref)))
+    assert (np.abs(f(got[rows]) - ref) <= tol).all()
 
 
 # ---------------------------------------------------------------- together
