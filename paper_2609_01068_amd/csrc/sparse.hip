@@ -87,16 +87,18 @@ constexpr int pow2_at_least(int g) { return g <= 1 ? 1 : g <= 2 ? 2 : g <= 4 ? 4
 
 // Scores for rows r .. r + nr - 1 of one slot and KV head g, by one wave:
 // sc[j * ld + b] of row j and page b (where it is a candidate), for `len` pages
-// (at most 64, a multiple of 16) from p0 on, from p0 + step on, .. below p1.
+// (at most 16 U, a multiple of 16) from p0 on, from p0 + step on, .. below p1.
 // Returns the largest sum |q k| that this lane saw, as bits.
 //
 // bf16: v_mfma_f32_16x16x32_bf16 with the queries as A (rows: row j's head h
 // at j GP + h, GP the group rounded up to a power of two with the last head
 // repeated) and 16 pages as B; a lane then holds four heads of one page and
 // the group's maximum takes at most two lane exchanges.  The same product of
-// absolute values gives the bound.  A wave takes 64 pages at a time: one
-// coalesced read of their ids, then 16 loads in flight.
-template <int HD, int GP>
+// absolute values gives the bound.  A wave takes 16 U pages at a time: one
+// coalesced read of their ids, then 4 U loads in flight (fused form, 512 rows:
+// 62 us with U = 2, which leaves registers for more waves, 65 with 4; split
+// form, 445 rows: 61 and 59).
+template <int HD, int GP, int U>
 __device__ __forceinline__ uint32_t score_pages_bf16(const SelectArgs& a, int r, int nr, int g, int p0, int len, int step,
                                                      int p1, float* sc, int64_t ld) {
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
@@ -105,7 +107,7 @@ __device__ __forceinline__ uint32_t score_pages_bf16(const SelectArgs& a, int r,
     const int32_t* row = a.c.page_table + static_cast<int64_t>(a.row_slot[r]) * a.c.max_pages;
     auto ids = [&](int p) { return lane < len && p + lane < p1 ? row[p + lane] : -1; };
     int next = ids(p0);
-    bf16x8 qf[HD / 32], qm[HD / 32];
+    bf16x8 qf[HD / 32];
     {
         const int j = min(col / GP, nr - 1), h = min(col % GP, a.G - 1);
         const __bf16* src = q + (r + j) * a.ldq + (static_cast<int64_t>(g) * a.G + h) * HD + 8 * grp;
@@ -122,8 +124,6 @@ __device__ __forceinline__ uint32_t score_pages_bf16(const SelectArgs& a, int r,
                 x = *reinterpret_cast<const uint4*>(e);
             }
             qf[b] = __builtin_bit_cast(bf16x8, x);
-            x.x &= 0x7FFF7FFFu; x.y &= 0x7FFF7FFFu; x.z &= 0x7FFF7FFFu; x.w &= 0x7FFF7FFFu;
-            qm[b] = __builtin_bit_cast(bf16x8, x);
         }
     }
     // last candidates of the rows this lane stores
@@ -141,16 +141,16 @@ __device__ __forceinline__ uint32_t score_pages_bf16(const SelectArgs& a, int r,
         int id = next;
         next = ids(p + step);
         if (id >= a.c.num_pages) id = -1;
-        u32x4 kf[4][HD / 32];
+        u32x4 kf[U][HD / 32];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int64_t page = max(__shfl(id, 16 * u + (lane >> 2), 64), 0);
             const __bf16* src = keys + (page * a.c.n_kv + g) * HD + 8 * (lane & 3);
 #pragma unroll
             for (int b = 0; b < HD / 32; ++b) kf[u][b] = *reinterpret_cast<const u32x4*>(src + 32 * b);
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < U; ++u) {
             if (16 * u >= len || p + 16 * u >= p1) break;
             f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f}, m = s;
 #pragma unroll
@@ -158,7 +158,8 @@ __device__ __forceinline__ uint32_t score_pages_bf16(const SelectArgs& a, int r,
                 u32x4 x = to_product(kf[u][b], from);
                 s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[b], __builtin_bit_cast(bf16x8, x), s, 0, 0, 0);
                 x &= 0x7FFF7FFFu;
-                m = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qm[b], __builtin_bit_cast(bf16x8, x), m, 0, 0, 0);
+                const u32x4 qa = __builtin_bit_cast(u32x4, qf[b]) & 0x7FFF7FFFu;
+                m = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qa), __builtin_bit_cast(bf16x8, x), m, 0, 0, 0);
             }
             const int b = p + 16 * u + col;
             const bool there = __shfl(id, 16 * u + col, 64) >= 0;
@@ -228,10 +229,10 @@ __device__ __forceinline__ uint32_t score_pages_f32(const SelectArgs& a, int r, 
     return big;
 }
 
-template <typename T, int HD, int GP>
+template <typename T, int HD, int GP, int U>
 __device__ __forceinline__ uint32_t score_pages(const SelectArgs& a, int r, int nr, int g, int p0, int len, int step, int p1,
                                                 float* sc, int64_t ld) {
-    if constexpr (sizeof(T) == 2) return score_pages_bf16<HD, GP>(a, r, nr, g, p0, len, step, p1, sc, ld);
+    if constexpr (sizeof(T) == 2) return score_pages_bf16<HD, GP, U>(a, r, nr, g, p0, len, step, p1, sc, ld);
     else return score_pages_f32<HD>(a, r, nr, g, p0, len, step, p1, sc, ld);
 }
 
@@ -619,7 +620,7 @@ block_select_fused(SelectArgs a) {
         __syncthreads();
         // equal shares of 16 pages; a wave's part begins where the last one's ends
         const int first = a.sink, end = most - a.local, tiles = (end - first + 15) / 16;
-        const uint32_t big = score_pages<T, HD, GP>(a, r, nr, g, first + 16 * (tiles * w / NW), kUnit, kUnit,
+        const uint32_t big = score_pages<T, HD, GP, 2>(a, r, nr, g, first + 16 * (tiles * w / NW), 32, 32,
                                                     min(first + 16 * (tiles * (w + 1) / NW), end), sc, ld);
         if (big) atomicMax(&bound, big);
         __syncthreads();
@@ -649,7 +650,7 @@ block_scores(SelectArgs a) {
     int most = 0;
     for (int j = 0; j < nr; ++j) most = max(most, visible_pages(a, r + j));
     if (most <= a.top_k) return;
-    uint32_t big = score_pages<T, HD, GP>(a, r, nr, g, blockIdx.x * kUnit, kUnit, slices * kUnit, most - a.local,
+    uint32_t big = score_pages<T, HD, GP, kUnit / 16>(a, r, nr, g, blockIdx.x * kUnit, kUnit, slices * kUnit, most - a.local,
                                           a.scores + (static_cast<int64_t>(r) * a.c.n_kv + g) * a.ld,
                                           static_cast<int64_t>(a.c.n_kv) * a.ld);
 #pragma unroll
