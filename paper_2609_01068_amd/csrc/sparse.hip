@@ -37,8 +37,8 @@ __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_ex
 // computed for every page: scores in 32 bits (matrix instructions for bf16)
 // come with a bound on their error, and only pages closer to the border than
 // that bound are scored again in 64 bits.  The first pass is then bound by
-// reading the block keys; at the sizes of a 512-request step (263 candidate
-// pages, 59 wanted) one row in eight scores two or three pages again.
+// reading the block keys; in the 512-row step (normal keys and queries, 260
+// candidate pages, 59 wanted) one row in nine scores two pages again.
 //
 // Error of a 32-bit score: sums of at most 128 products, each step off by at
 // most 2^-23 of the partial sum's magnitude, hence by 2^-16 sum |q k|; 2^-14
@@ -587,7 +587,7 @@ __device__ __forceinline__ void pick_all(const SelectArgs& a, int r, int g, int 
 // Tables up to this many pages take the fused form (512 rows of 264 pages on
 // average: 55 us, 86 split; 64 rows of 750: 30 and 32; 8 rows: 19 and 15).
 constexpr int kFusedPages = 1024;
-constexpr int kPickLdsPages = 12288; // scores of a row that the split form copies to LDS (48 KB)
+constexpr int kPickLdsPages = 12288; // padded scores of a row that the split form copies to LDS (48 KB)
 constexpr int kUnit = 64;            // pages that a wave scores at a time
 
 // A KV head's part of a block key (256 bytes at 128 channels) falls on few of
@@ -1033,7 +1033,7 @@ template <int HD>
 __device__ __forceinline__ bool attend_tile(const AttendArgs& a, int64_t r, int nr, int g, float* buf, float* sm,
                                             float* sl) {
     constexpr int NW = kAttendWaves;
-    __shared__ int n_list, odd;
+    __shared__ int n_list;
     const KvPages& c = a.c;
     const int G = a.G, tid = threadIdx.x;
     const int lane = tid & 63, w = tid >> 6, col = lane & 15, grp = lane >> 4;
@@ -1041,7 +1041,7 @@ __device__ __forceinline__ bool attend_tile(const AttendArgs& a, int64_t r, int 
     uint32_t* mask = reinterpret_cast<uint32_t*>(buf);               // 16 bits a page: rows that select it
     int32_t* list = reinterpret_cast<int32_t*>(buf) + words;
     for (int i = tid; i < words; i += 64 * NW) mask[i] = 0;
-    if (tid == 0) n_list = odd = 0;
+    if (tid == 0) n_list = 0;
     __syncthreads();
     bool twice = false;
     int last = -1;                                                   // newest position of the tile
