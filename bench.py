@@ -144,11 +144,27 @@ def weight_bytes(W) -> float:
     return float(total)
 
 
-def measure_decode(seed: int, steps: int, warmup: int, attn_gate: bool = False):
+SPARSE_SINK, SPARSE_LOCAL = 1, 4      # pages that a sparse step always reads, first and last
+
+
+def sparse_step_keys(lens, top_k: int):
+    """(tokens attended to, block keys read) per KV head of one sparse step
+    over caches of ``lens`` tokens, the step's included."""
+    keys = scored = 0
+    for n in lens:
+        pages = -(-int(n) // 16)
+        keys += int(n) if pages <= top_k else (top_k - 1) * 16 + (int(n) - 1) % 16 + 1
+        scored += pages - SPARSE_SINK - SPARSE_LOCAL if pages > top_k else 0
+    return keys, scored
+
+
+def measure_decode(seed: int, steps: int, warmup: int, attn_gate: bool = False, sparse_pages: int = 0):
     """Dynamic re-prediction at scale: 512 in-flight
     requests whose paged draft KV caches hold U[256, 8192] prompt tokens
     (filled by untimed prefill calls), then ``steps`` timed decode steps of
-    one new token per request.  Returns the measurement as a dict."""
+    one new token per request.  Returns the measurement as a dict.
+    ``sparse_pages``: attend to so many pages per request and KV head only
+    (0: to every cached token)."""
     import numpy as np
     import torch
     from paper_2609_01068_amd.predictor import OutletsPredictor
@@ -167,6 +183,8 @@ def measure_decode(seed: int, steps: int, warmup: int, attn_gate: bool = False):
     pred = OutletsPredictor(wl.shape, wl.weight_fmt, wl.act_fmt, W, max_slots=B, max_seq_len=max_seq,
                             num_pages=pages, max_batch_tokens=max_chunk_tokens, max_batch_requests=B)
     del W
+    if sparse_pages:
+        pred.sparse_steps(sparse_pages, SPARSE_SINK, SPARSE_LOCAL)
     print(f"[bench] filling {B} KV caches ({int(lens.sum())} tokens) with prefill calls", file=sys.stderr, flush=True)
     for i in range(0, B, chunk):
         idx = list(range(i, min(B, i + chunk)))
@@ -208,6 +226,12 @@ def measure_decode(seed: int, steps: int, warmup: int, attn_gate: bool = False):
     ms_per_step = max(gpu_ms, wall * 1e3) / steps
     # keys read per step: every cached token of every request plus the new one
     keys = sum(cached0 + B * (t + 1) for t in range(steps)) / steps
+    scored = 0
+    if sparse_pages:
+        # per step: the selected pages' tokens, and the block keys of the others (half of K and V)
+        per = [sparse_step_keys([int(n) + warmup + t + 1 for n in lens], sparse_pages) for t in range(steps)]
+        keys, scored = (sum(x) / steps for x in zip(*per))
+        keys += scored / 2
     kv_bytes = keys * wl.shape.n_kv * wl.shape.head_dim * 2 * 2
     attn_ms = prof["ATTN"][0] / max(1, prof["ATTN"][1])
     attn_gbs = kv_bytes / (attn_ms * 1e-3) / 1e9
@@ -216,9 +240,11 @@ def measure_decode(seed: int, steps: int, warmup: int, attn_gate: bool = False):
     return {
         "wl": wl, "requests": B, "steps": steps, "warmup": warmup, "ms_per_step": ms_per_step,
         "draft_tokens_per_s": B / (ms_per_step / 1e3), "cached_tokens_at_start": cached0,
-        "attn": {"kernel": "decode attention over the paged KV cache", "bound": "hbm", "achieved": attn_gbs,
+        "attn": {"kernel": "sparse attention and its page selection" if sparse_pages else
+                 "decode attention over the paged KV cache", "bound": "hbm", "achieved": attn_gbs,
                  "peak": PEAK_HBM_GBS, "unit": "GB/s", "frac": attn_gbs / PEAK_HBM_GBS,
-                 "traffic": recorded_traffic("decode_attention_8b_b512.md", "attn.hip", "attn"),
+                 "traffic": None if sparse_pages else
+                 recorded_traffic("decode_attention_8b_b512.md", "attn.hip", "attn"),
                  "bytes_per_launch": kv_bytes, "avg_ms": attn_ms},
         "step": {"bound": "hbm", "achieved": step_gbs, "peak": PEAK_HBM_GBS, "unit": "GB/s",
                  "frac": step_gbs / PEAK_HBM_GBS, "bytes_per_step": step_bytes, "kv_bytes_per_step": kv_bytes,
@@ -229,14 +255,15 @@ def measure_decode(seed: int, steps: int, warmup: int, attn_gate: bool = False):
 
 def bench_decode(a):
     """The 512-request decode steps as the bench line itself."""
-    m = measure_decode(a.seed, a.steps, a.warmup, a.attn_gate)
+    m = measure_decode(a.seed, a.steps, a.warmup, a.attn_gate, a.sparse_pages)
     out = {
         "metric": METRIC, "value": m["draft_tokens_per_s"], "unit": "draft tokens/s (request-steps/s)",
         "n_gpus": 1, "steps": a.steps, "warmup": a.warmup, "ms_per_step": m["ms_per_step"],
         "higher_is_better": True, "scaling": "weak", "vs_baseline": None, "dtype": "bf16",
         "data": "synthetic (seeded on device; U[256,8192] cached prompt tokens; fresh N(0,1) x (1,4,16) states per step)",
         "config": {"workload": DECODE_WORKLOAD, "requests": m["requests"],
-                   "cached_tokens_at_start": m["cached_tokens_at_start"], "attn_gate": m["wl"].attn_gate},
+                   "cached_tokens_at_start": m["cached_tokens_at_start"], "attn_gate": m["wl"].attn_gate,
+                   "sparse_pages": a.sparse_pages},
         "roofline": m["attn"],
         "step_hbm": m["step"],
         "kernels_step": m["kernels_step"],
@@ -480,6 +507,9 @@ def main(argv=None):
     ap.add_argument("--input-embed", action="store_true",
                     help="prefill-8b: draft layer with EAGLE-3 input embeddings (QKV over [emb ; f_ctx], "
                          "V = 128,256 embedding table)")
+    ap.add_argument("--sparse-pages", type=int, default=0,
+                    help="decode-8b: sparse steps of so many 16-token pages per request and KV head "
+                         "(0: attend to every cached token)")
     ap.add_argument("--copy-probe", action="store_true",
                     help="only run a plain 1 GiB device-to-device copy (3 times); used to scale "
                          "rocprof's FETCH_SIZE / WRITE_SIZE counters to bytes")
@@ -491,6 +521,11 @@ def main(argv=None):
 
     if a.input_embed and a.workload != "prefill-8b":
         print("--input-embed is measured on the prefill-8b workload only", file=sys.stderr)
+        return 2
+
+    if a.sparse_pages and (a.workload != "decode-8b" or a.sparse_pages < SPARSE_SINK + SPARSE_LOCAL):
+        print(f"--sparse-pages is measured on the decode-8b workload only, from {SPARSE_SINK + SPARSE_LOCAL} pages on",
+              file=sys.stderr)
         return 2
 
     if a.workload == "sched-1p3d":

@@ -424,15 +424,18 @@ void write_rows(const KvPages& c, int n_rows, const int32_t* slot_map, const voi
 #undef OUTLETS_WRITE
 }
 
-// Rows that end a page average its 16 keys: a wave looks at 64 rows and takes
-// those pages one after another, all of a page's keys in flight.
+// Rows that end a page average its 16 keys: a wave looks at kKeyRows rows (a
+// prompt's end one page among them) and takes those pages one after another,
+// all of a page's keys in flight.
+constexpr int kKeyRows = 16;
+
 template <typename T, int HD>
 __global__ void __launch_bounds__(64)
 block_keys_kernel(KvPages c, int n_rows, const int32_t* __restrict__ row_slot, const int32_t* __restrict__ positions) {
     typedef T T2 __attribute__((ext_vector_type(2)));
-    const int g = blockIdx.x, lane = threadIdx.x, r = blockIdx.y * 64 + lane, ch = 2 * lane;
+    const int g = blockIdx.y, lane = threadIdx.x, r = blockIdx.x * kKeyRows + lane, ch = 2 * lane;
     int page = -1;
-    if (r < n_rows) {
+    if (lane < kKeyRows && r < n_rows) {
         const int pos = positions[r], slot = row_slot[r];
         if (pos >= 0 && pos % kPage == kPage - 1 && pos / kPage < c.max_pages && slot >= 0 && slot < c.max_slots)
             page = c.page_table[static_cast<int64_t>(slot) * c.max_pages + pos / kPage];
@@ -502,7 +505,7 @@ void launch_cache_write(const KvPages& c, int n_rows, const int32_t* slot_map, c
 void launch_block_keys(const KvPages& c, int n_rows, const int32_t* row_slot, const int32_t* positions,
                        hipStream_t st) {
     if (n_rows <= 0) return;
-    const dim3 grid(c.n_kv, (n_rows + 63) / 64), block(64);
+    const dim3 grid((n_rows + kKeyRows - 1) / kKeyRows, c.n_kv), block(64);
 #define OUTLETS_KEYS(T, HD) \
     hipLaunchKernelGGL((block_keys_kernel<T, HD>), grid, block, 0, st, c, n_rows, row_slot, positions)
     if (c.fmt == OUTLETS_FMT_F32) {

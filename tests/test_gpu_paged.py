@@ -144,10 +144,8 @@ def test_large_batches(n, n_rows):
 ])
 @pytest.mark.parametrize("rows_more", [0, 5000])
 def test_refused_appends_change_nothing(slots, new, n_rows, rc, rows_more):
-    if rows_more and n_rows == 9:
-        if slots == [0, 2]:
-            pytest.skip("the rows suffice")
-    n_rows += rows_more
+    if slots != [0, 2]:                                 # (too few rows: more would suffice)
+        n_rows += rows_more
     pt = tables(11, 4, 100)
     pt.append(i32([1]), i32([30]), 30)
     was = snapshot(pt)
@@ -744,7 +742,8 @@ def test_select_of_denormal_and_huge_values():
         q = randn((1, n_kv * G, hd), fmt, 4) * scale
         kv = cache_over(table, 101, n_kv, hd, fmt, block_keys=k)
         got = kv.select(q, i32(slots), i32([1599]), top_k, 1, 2).cpu().numpy()
-        want = plain_select(k.double().cpu().numpy(), q.double().cpu().numpy(), table, slots, [1599], n_kv, top_k, 1, 2)
+        with np.errstate(invalid="ignore"):             # the largest queries are infinite
+            want = plain_select(k.double().cpu().numpy(), q.double().cpu().numpy(), table, slots, [1599], n_kv, top_k, 1, 2)
         assert np.array_equal(got, want), fmt
 
 
