@@ -1008,7 +1008,7 @@ int outlets_create(const outlets_config* cfg, const outlets_weights* weights, in
     return OUTLETS_OK;
 }
 
-int outlets_sparse_steps(outlets_ctx* ctx, int32_t top_k, int32_t sink, int32_t local) {
+int outlets_sparse_steps(outlets_ctx* ctx, int32_t top_k, int32_t sink, int32_t local) try {
     if (!ctx) return fail(OUTLETS_ERR_INVALID_ARG, "null context");
     if (top_k == 0) {
         ctx->sparse_top = 0;
@@ -1044,6 +1044,8 @@ int outlets_sparse_steps(outlets_ctx* ctx, int32_t top_k, int32_t sink, int32_t 
     ctx->sparse_local = local;
     ctx->sparse_top = top_k;
     return OUTLETS_OK;
+} catch (...) {    // host memory for a message or a list
+    return OUTLETS_ERR_NOMEM;
 }
 
 int outlets_destroy(outlets_ctx* ctx) {
