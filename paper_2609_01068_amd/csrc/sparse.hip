@@ -55,6 +55,8 @@ struct SelectArgs {
     int64_t ldq;
     int n_rows, G, top_k, sink, local;
     int tile;              // rows scored together where they belong to one slot
+    int cap;               // tiles of up to so many pages are the fused form's, others the split form's
+    int lds;               // scores of a row in LDS (fused form)
     int ld;                // scores of a row: max_pages, to a multiple of kPad
     uint64_t* keys;        // [rows, n_kv, ld]: 64-bit scores of crowded borders
     float* scores;         // [rows, n_kv, ld] (split form)
@@ -81,6 +83,16 @@ template <typename Args> __device__ __forceinline__ int block_rows(const Args& a
     for (int i = r0 + 1; i < r1; ++i) same = same && a.row_slot[i] == a.row_slot[r0];
     if (!same) return 1;
     return r == r0 ? r1 - r0 : 0;
+}
+
+// Most pages that a row of r's tile sees, where the tile's rows share a slot,
+// or that row r sees.
+__device__ __forceinline__ int tile_pages(const SelectArgs& a, int r) {
+    const int r0 = r / a.tile * a.tile, nr = block_rows(a, r0);
+    if (nr == 1 && r != r0) return visible_pages(a, r);
+    int most = 0;
+    for (int j = 0; j < nr; ++j) most = max(most, visible_pages(a, r0 + j));
+    return most;
 }
 
 constexpr int pow2_at_least(int g) { return g <= 1 ? 1 : g <= 2 ? 2 : g <= 4 ? 4 : g <= 8 ? 8 : 16; }
@@ -604,10 +616,10 @@ template <typename T, int HD, int GP>
 __global__ void __launch_bounds__(256)
 block_select_fused(SelectArgs a) {
     constexpr int NW = 4;
-    extern __shared__ float sc[];                    // [tile][ld]
+    extern __shared__ float sc[];                    // [tile][lds]
     __shared__ PickShared<64> sh[NW];
     __shared__ uint32_t bound;
-    const int w = threadIdx.x >> 6, ld = a.ld;
+    const int w = threadIdx.x >> 6, ld = a.lds;
     const int x = blockIdx.x % 8, y = blockIdx.x / 8, g = y % a.c.n_kv;
     const int r = (y / a.c.n_kv * 8 + x) * a.tile + blockIdx.y;
     if (r >= a.n_rows) return;
@@ -615,6 +627,7 @@ block_select_fused(SelectArgs a) {
     if (nr == 0) return;
     int most = 0;
     for (int j = 0; j < nr; ++j) most = max(most, visible_pages(a, r + j));
+    if (most > a.cap) return;
     if (most > a.top_k) {                            // uniform over the block
         if (threadIdx.x == 0) bound = 0;
         __syncthreads();
@@ -630,7 +643,7 @@ block_select_fused(SelectArgs a) {
         if (nb <= a.top_k) pick_all<64>(a, r + j, g, nb);
         else
             pick_row<T, HD, 64>(a, r + j, g, nb, sc + j * ld, __uint_as_float(bound),
-                                a.keys + (static_cast<int64_t>(r + j) * a.c.n_kv + g) * ld, sh[w]);
+                                a.keys + (static_cast<int64_t>(r + j) * a.c.n_kv + g) * a.ld, sh[w]);
     }
 }
 
@@ -649,7 +662,7 @@ block_scores(SelectArgs a) {
     if (nr == 0) return;
     int most = 0;
     for (int j = 0; j < nr; ++j) most = max(most, visible_pages(a, r + j));
-    if (most <= a.top_k) return;
+    if (most <= a.cap || most <= a.top_k) return;
     uint32_t big = score_pages<T, HD, GP, kUnit / 16>(a, r, nr, g, blockIdx.x * kUnit, kUnit, slices * kUnit, most - a.local,
                                           a.scores + (static_cast<int64_t>(r) * a.c.n_kv + g) * a.ld,
                                           static_cast<int64_t>(a.c.n_kv) * a.ld);
@@ -666,6 +679,7 @@ block_pick(SelectArgs a, int slices) {
     __shared__ PickShared<NT> sh;
     __shared__ uint32_t bound;
     const int g = blockIdx.x, r = blockIdx.y, nb = visible_pages(a, r);
+    if (a.cap >= 0 && tile_pages(a, r) <= a.cap) return;
     if (nb <= a.top_k) {
         pick_all<NT>(a, r, g, nb);
         return;
@@ -1235,12 +1249,19 @@ void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int
     // every row sees all it may read: no scores, no workspace
     const bool plain = c.max_pages <= top_k;
     const bool fused = plain || c.max_pages <= kFusedPages;
-    const int ld = score_stride(c);
+    // Long tables and many rows, more or less one of each slot (a decode step):
+    // the rows whose caches are short take the fused form all the same
+    // (8 heads of 512 rows of 264 pages at the mean, in tables of 2,048 and 8,192:
+    // 90 and 158 us by the split form alone, 74 and 115 by both).
+    const bool both =
+        !fused && rows.n_rows < 2 * c.max_slots && static_cast<int64_t>(rows.n_rows) * c.n_kv >= 4 * cus;
+    const int cap = plain ? c.max_pages : fused || both ? kFusedPages : -1;
+    const int ld = score_stride(c), lds_row = std::min(ld, kFusedPages);
     const int slab = static_cast<int>(std::min<int64_t>(plain ? rows.n_rows : ws_bytes / row_bytes,
                                                         std::min(rows.n_rows, 32768)));     // (the grid's z)
     int tile = plain ? 1 : 16 / gp;
-    if (fused)
-        while (tile > 1 && tile * ld * 4 > kFusedBytes) tile /= 2;
+    if (fused || both)
+        while (tile > 1 && tile * lds_row * 4 > kFusedBytes) tile /= 2;
     for (int r0 = 0; r0 < rows.n_rows; r0 += slab) {
         const int n = std::min(slab, rows.n_rows - r0);
         const int64_t items = static_cast<int64_t>(n) * c.n_kv;
@@ -1248,28 +1269,28 @@ void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int
         float* scores = plain ? nullptr : reinterpret_cast<float*>(keys + items * ld);
         const SelectArgs a{c,     rows.row_slot + r0, rows.positions + r0,
                            static_cast<const char*>(rows.q) + eb * rows.ldq * r0,
-                           rows.ldq, n, G, top_k, sink, local, tile, ld, keys, scores,
+                           rows.ldq, n, G, top_k, sink, local, tile, cap, lds_row, ld, keys, scores,
                            plain ? nullptr : scores + items * ld, sel + static_cast<int64_t>(r0) * c.n_kv * top_k};
 #define OUTLETS_SELECT(T, HD, GP)                                                                                 \
     do {                                                                                                          \
         const dim3 blocks((n + 8 * tile - 1) / (8 * tile) * 8 * c.n_kv, tile);                                    \
-        const size_t lds = plain ? 0 : sizeof(float) * tile * ld;                                        \
-        if (fused) {                                                                                              \
-            hipLaunchKernelGGL((block_select_fused<T, HD, GP>), blocks, dim3(256), lds, st, a);                     \
-        } else {                                                                                                  \
-            hipLaunchKernelGGL((block_scores<T, HD, GP>), dim3(slices, c.n_kv, n), dim3(64), 0, st, a); \
-            if (items < cus) OUTLETS_PICK(T, HD, 1024);                                                            \
-            else if (items < 4 * cus) OUTLETS_PICK(T, HD, 256);                                                    \
-            else OUTLETS_PICK(T, HD, 64);                                                                          \
+        const size_t lds = plain ? 0 : sizeof(float) * tile * lds_row;                                            \
+        if (fused || both)                                                                                        \
+            hipLaunchKernelGGL((block_select_fused<T, HD, GP>), blocks, dim3(256), lds, st, a);                   \
+        if (!fused) {                                                                                             \
+            hipLaunchKernelGGL((block_scores<T, HD, GP>), dim3(slices, c.n_kv, n), dim3(64), 0, st, a);           \
+            if (items < cus) OUTLETS_PICK(T, HD, 1024);                                                           \
+            else if (items < 4 * cus) OUTLETS_PICK(T, HD, 256);                                                   \
+            else OUTLETS_PICK(T, HD, 64);                                                                         \
         }                                                                                                         \
     } while (0)
 #define OUTLETS_PICK(T, HD, NT)                                                                                   \
     do {                                                                                                          \
-        if (ld <= kPickLdsPages)                                                                         \
-            hipLaunchKernelGGL((block_pick<T, HD, NT, true>), dim3(c.n_kv, n), dim3(NT), sizeof(float) * ld, st, \
+        if (ld <= kPickLdsPages)                                                                                  \
+            hipLaunchKernelGGL((block_pick<T, HD, NT, true>), dim3(c.n_kv, n), dim3(NT), sizeof(float) * ld, st,  \
                                a, slices);                                                                        \
         else                                                                                                      \
-            hipLaunchKernelGGL((block_pick<T, HD, NT, false>), dim3(c.n_kv, n), dim3(NT), 0, st, a, slices);          \
+            hipLaunchKernelGGL((block_pick<T, HD, NT, false>), dim3(c.n_kv, n), dim3(NT), 0, st, a, slices);      \
     } while (0)
 #define OUTLETS_SELECT_G(HD)                                                                                      \
     switch (gp) {                                                                                                 \

@@ -519,6 +519,30 @@ def test_select_long_and_shared(fmt, G, lens):
 
 # ---------------------------------------------------------------- attention
 
+@pytest.mark.parametrize("fmt,G", [("f32", 2), ("bf16", 1), ("bf16", 4), ("bf16", 16)])
+@pytest.mark.parametrize("parts", [1, 3])
+def test_select_short_rows_of_long_tables(monkeypatch, fmt, G, parts):
+    """Tables of more than 1,024 pages, and rows of fewer, of as many and of
+    more; alone, side by side with a row of the same slot, and with none to see."""
+    from paper_2609_01068_amd import paged
+    n_kv, hd, n, slots, width, top_k = 8, 64, 171, 128, 1300, 24
+    r = np.random.default_rng(G)
+    table = r.integers(0, 2000, size=(slots, width)).astype(np.int32)
+    pages = r.choice([1, 24, 25, 90, 300, 1023, 1024, 1025, 1300], size=n)
+    rs = r.integers(0, slots, size=n).astype(np.int32)
+    rs[16:48], rs[64:71], rs[-3:] = 5, 7, 9
+    pages[32:48] = np.minimum(pages[32:48], 1024)
+    pos = (pages * PAGE - 1 - r.integers(0, PAGE, size=n)).astype(np.int32)
+    rs[3], pos[20], rs[50], pos[60] = -1, -1, slots, width * PAGE
+    keys, q = randn((2000, n_kv, hd), fmt, 3, 0.3), randn((n, n_kv * G, hd), fmt, 4)
+    kv = cache_over(table, 2000, n_kv, hd, fmt, block_keys=keys)
+    if parts > 1:
+        monkeypatch.setattr(paged, "_SELECT_WS", n * n_kv * width * 12 // parts)
+    want = plain_select(keys.double().cpu().numpy(), q.double().cpu().numpy(), table, rs, pos, n_kv, top_k, 1, 3)
+    for _ in range(2):
+        assert np.array_equal(kv.select(q, i32(rs), i32(pos), top_k, 1, 3).cpu().numpy(), want)
+
+
 def attention_ref(kp, vp, q, table, row_slot, pos, sel, gate):
     """Output and error bound (without the rounding of bf16) in numpy float64."""
     n, n_q, hd = q.shape
