@@ -1244,7 +1244,7 @@ constexpr int kFusedBytes = 16 << 10;    // LDS of a block's scores in the fused
 
 void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int sink, int local, int32_t* sel, void* ws,
                          int64_t ws_bytes, int cus, hipStream_t st) {
-    const int G = rows.n_q / c.n_kv, gp = pow2_at_least(G), slices = score_slices(c);
+    const int G = rows.n_q / c.n_kv, gp = pow2_at_least(G);
     const int64_t eb = c.fmt == OUTLETS_FMT_F32 ? 4 : 2, row_bytes = block_select_ws(c, 1);
     // every row sees all it may read: no scores, no workspace
     const bool plain = c.max_pages <= top_k;
@@ -1252,9 +1252,13 @@ void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int
     // Long tables and many rows, more or less one of each slot (a decode step):
     // the rows whose caches are short take the fused form all the same
     // (8 heads of 512 rows of 264 pages at the mean, in tables of 2,048 and 8,192:
-    // 90 and 158 us by the split form alone, 74 and 115 by both).
+    // 90 and 158 us by the split form alone, 74 and 102 by both).
     const bool both =
         !fused && rows.n_rows < 2 * c.max_slots && static_cast<int64_t>(rows.n_rows) * c.n_kv >= 4 * cus;
+    // many rows are waves enough: fewer blocks for those with nothing to score
+    // (the 512 rows in tables of 8,192: 115 us with 40 slices, 102 with 24, 97
+    // with 16; with a quarter of them at 8,191 pages: 701, 710, 724)
+    const int slices = both ? std::min(24, score_slices(c)) : score_slices(c);
     const int cap = plain ? c.max_pages : fused || both ? kFusedPages : -1;
     const int ld = score_stride(c), lds_row = std::min(ld, kFusedPages);
     const int slab = static_cast<int>(std::min<int64_t>(plain ? rows.n_rows : ws_bytes / row_bytes,
