@@ -70,6 +70,8 @@ def _on_stream(call):
     def wrapper(self, *args, stream=None, **kw):
         if stream is None:
             return call(self, *args, **kw)
+        if stream.device_index != self._index:
+            raise ValueError(f"stream must be one of cuda:{self._index}")
         with torch.cuda.stream(stream):
             return call(self, *args, **kw)
     return wrapper

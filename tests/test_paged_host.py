@@ -146,3 +146,22 @@ def test_empty_calls_need_no_gpu():
     assert write(cache(), n=0, sm=None, k=None, v=None) == B.OUTLETS_OK
     assert select(cache(), n=0, rs=None, pos=None, q=None, sel=None, ws=None) == B.OUTLETS_OK
     assert attend(cache(), n=0, rs=None, pos=None, q=None, sel=None, out=None, ws=None) == B.OUTLETS_OK
+
+
+def test_streams_of_other_devices_are_refused():
+    """One that is not the tables' would leave the call on the current stream."""
+    from paper_2609_01068_amd import paged
+
+    class Stream:
+        device_index = 1
+
+    tables = object.__new__(paged.PageTables)
+    tables._index = 0
+    for call in (tables.reset, lambda **kw: tables.append(None, None, 1, **kw), lambda **kw: tables.release(None, **kw)):
+        with pytest.raises(ValueError, match="cuda:0"):
+            call(stream=Stream())
+    kv = object.__new__(paged.PagedKV)
+    kv._index = 0
+    for call, n in ((kv.write, 3), (kv.select, 4), (kv.attend, 4)):
+        with pytest.raises(ValueError, match="cuda:0"):
+            call(*[None] * n, stream=Stream())
