@@ -823,8 +823,11 @@ __global__ void __launch_bounds__(HD) join_splits(AttendArgs a, int splits) {
 // rows that share pages waited for the L1's address path (219 cycles a page
 // and compute unit; 445 rows of 4 slots 134 us, now 121; 509
 // rows of their own 335 us, now 322).
-// Softmax statistics in fp32; the probabilities enter the second product as
-// bf16 and the row sum adds the same rounded values.
+// Softmax statistics in fp32; a probability enters the second product as the
+// sum of two bf16 values, 2^-16 off at most: as one value, 2^-8 off, it was as
+// large an error as the output's own rounding (one value and two, 509 rows of
+// 64 pages: 320 and 320 us, 6 rows of 128: 13.8 and 14.3, 445 rows of 4 slots:
+// 105 and 109).
 // ONCE: the pages are not read again soon (rows of different slots):
 // non-temporal loads, 509 rows of 64 pages 353 -> 335 us; where rows share
 // pages they cost (445 rows of 4 slots: 241 -> 270 us).
@@ -879,11 +882,13 @@ __device__ __forceinline__ void score_keys(const KeyFrag<HD>& f, const bf16x8* q
     }
 }
 
+// Probabilities as the B operand of the second product: hi + lo.
+struct Probs { bf16x8 hi, lo; };
+
 // The running softmax (m, l, o) of each column with the lane's eight scores: of
-// them the first `n` count (by column and page; 0 or less: none).  Returns the
-// probabilities, the B operand of the second product.
+// them the first `n` count (by column and page; 0 or less: none).
 template <int HD>
-__device__ __forceinline__ bf16x8 add_scores(int n, float qscale, float* s, float& m, float& l, f32x4* o) {
+__device__ __forceinline__ Probs add_scores(int n, float qscale, float* s, float& m, float& l, f32x4* o) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (i >= n) s[i] = -INFINITY;
@@ -904,11 +909,13 @@ __device__ __forceinline__ bf16x8 add_scores(int n, float qscale, float* s, floa
     }
     const float nm = m == -INFINITY ? 0.f : -m;
     float ps = 0.f;
-    bf16x8 pb;
+    Probs pb;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        pb[i] = static_cast<__bf16>(fast_exp2(fmaf(s[i], qscale, nm)));
-        ps += static_cast<float>(pb[i]);
+        const float p = fast_exp2(fmaf(s[i], qscale, nm));
+        pb.hi[i] = static_cast<__bf16>(p);
+        pb.lo[i] = static_cast<__bf16>(p - static_cast<float>(pb.hi[i]));
+        ps += p;
     }
     ps += __shfl_xor(ps, 16, 64);
     ps += __shfl_xor(ps, 32, 64);
@@ -917,9 +924,10 @@ __device__ __forceinline__ bf16x8 add_scores(int n, float qscale, float* s, floa
 }
 
 // `part`: some page holds fewer than its 16 tokens, `n` of the lane's eight
-// (what stands behind the newest token is not read).
+// (what stands behind the newest token is not read).  `both`: the second parts
+// of the probabilities too.
 template <int HD>
-__device__ __forceinline__ void add_values(const ValueFrag<HD>& f, bool part, int n, bf16x8 pb, f32x4* o) {
+__device__ __forceinline__ void add_values(const ValueFrag<HD>& f, bool part, int n, const Probs& pb, bool both, f32x4* o) {
 #pragma unroll
     for (int b = 0; b < HD / 16; ++b) {
         u32x4 x = f.x[b];
@@ -928,7 +936,8 @@ __device__ __forceinline__ void add_values(const ValueFrag<HD>& f, bool part, in
             for (int e = 0; e < 4; ++e)
                 x[e] &= (2 * e < n ? 0x0000FFFFu : 0u) | (2 * e + 1 < n ? 0xFFFF0000u : 0u);
         }
-        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), pb, o[b], 0, 0, 0);
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), pb.hi, o[b], 0, 0, 0);
+        if (both) o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), pb.lo, o[b], 0, 0, 0);
     }
 }
 
@@ -939,7 +948,7 @@ __device__ __forceinline__ void add_values(const ValueFrag<HD>& f, bool part, in
 // computed, the keys of the next one while its values are awaited.
 template <int HD, bool ONCE, typename Keys, typename Held>
 __device__ __forceinline__ void walk_pages(const KvPages& c, int g, uint64_t todo, int page, int idx, Keys keys, Held held,
-                                           float qscale, const bf16x8* qb, float& m, float& l, f32x4* o) {
+                                           float qscale, const bf16x8* qb, bool both, float& m, float& l, f32x4* o) {
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
     int a = 0, b = 0;
     bool two = false;
@@ -971,8 +980,8 @@ __device__ __forceinline__ void walk_pages(const KvPages& c, int g, uint64_t tod
             load_keys<HD, ONCE>(c, pa, pb, g, lane, kf);
         }
         const int half = 8 * (grp & 1);
-        const bf16x8 p = add_scores<HD>((grp >> 1 ? kb : ka) - half, qscale, s, m, l, o);
-        add_values<HD>(vf, min(ha, hb) < kPage, (grp >> 1 ? hb : ha) - half, p, o);
+        const Probs p = add_scores<HD>((grp >> 1 ? kb : ka) - half, qscale, s, m, l, o);
+        add_values<HD>(vf, min(ha, hb) < kPage, (grp >> 1 ? hb : ha) - half, p, both, o);
         if (!more) break;
     }
 }
@@ -1009,12 +1018,17 @@ __device__ __forceinline__ void attend_row(const AttendArgs& a, int64_t r, int g
     const int32_t* sel = a.sel + (r * c.n_kv + g) * top_k;
     bf16x8 qb[HD / 32];
     load_query<HD>(a, r, g, min(col, G - 1), col < G, grp, qb);
-    float m = -INFINITY, l = 0.f;
+    float m, l;
     f32x4 o[HD / 16];
+    // an infinite value times a second part that is 0 or negative is NaN or of the
+    // other sign: a wave whose sums are not finite walks again with the first
+    // parts alone
+    for (bool both = true;; both = false) {
+        m = -INFINITY;
+        l = 0.f;
 #pragma unroll
-    for (int b = 0; b < HD / 16; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (row) {
-        for (int e0 = 0; e0 < top_k; e0 += 64 * turn) {
+        for (int b = 0; b < HD / 16; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int e0 = 0; row && e0 < top_k; e0 += 64 * turn) {
             // 64 entries of this wave, one a lane; entries that are no visible
             // page of the row are dropped here
             const int e = e0 + lane * turn + first;
@@ -1023,8 +1037,14 @@ __device__ __forceinline__ void attend_row(const AttendArgs& a, int64_t r, int g
             if (idx >= 0 && idx <= pos / kPage) page = row[idx];
             if (page >= c.num_pages) page = -1;
             auto tokens = [&](int i) { return pos + 1 - i * kPage; };
-            walk_pages<HD, ONCE>(c, g, __ballot(page >= 0), page, idx, tokens, tokens, a.qscale, qb, m, l, o);
+            walk_pages<HD, ONCE>(c, g, __ballot(page >= 0), page, idx, tokens, tokens, a.qscale, qb, both, m, l, o);
         }
+        bool finite = true;
+#pragma unroll
+        for (int b = 0; b < HD / 16; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) finite = finite && fabsf(o[b][e]) < INFINITY;
+        if (!both || __all(finite || col >= G)) break;
     }
     if (col < G) {
         if (grp == 0) { sm[w * kMaxGroup + col] = m; sl[w * kMaxGroup + col] = l; }
@@ -1095,7 +1115,7 @@ __device__ __forceinline__ bool attend_tile(const AttendArgs& a, int64_t r, int 
         walk_pages<HD, false>(
             c, g, __ballot(page >= 0), page, idx,
             [&](int i) { return mask[i >> 1] >> (16 * (i & 1) + j) & 1u ? pos + 1 - i * kPage : 0; },
-            [&](int i) { return last + 1 - i * kPage; }, a.qscale, qb, m, l, o);
+            [&](int i) { return last + 1 - i * kPage; }, a.qscale, qb, true, m, l, o);
     }
     __syncthreads();                                                 // the masks and the list are done with
     if (mine) {
