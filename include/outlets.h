@@ -468,7 +468,9 @@ int64_t outlets_block_select_workspace(const outlets_kv_pages* cache, int32_t n_
  * `sel` that are no page the row sees (-1, above positions[r] / 16, not in
  * the table) are skipped; an entry given twice counts twice; a row without
  * tokens gives zeros.  What the pages hold behind the row's position is not
- * used.
+ * used.  The same call gives the same bits; a row's sums are taken in another
+ * order beside other rows of its slot, or in a call of fewer rows, so its last
+ * bits may differ there.
  *   q as above, rows 16-byte aligned (else UNSUPPORTED).
  *   gate (nullable): laid out like q with its own stride; output element x is
  *     multiplied by sigmoid(gate x) (the attention output gate).

@@ -1062,12 +1062,14 @@ __device__ __forceinline__ void attend_row(const AttendArgs& a, int64_t r, int g
 // with nothing that counts written, where that is not the same as row by row:
 // a list that names a page twice, or an output that is not finite (a value of a
 // page that only other rows select may be infinite or NaN, and 0 times it is
-// not 0).  LDS: `buf` holds the pages' row masks and their list, then the states.
+// not 0).  The pages are taken in their order, whatever the order in which the
+// rows' entries arrive, so that a call repeats its bits.  LDS: `buf` holds the
+// pages' row masks and their list, then the states.
 template <int HD>
 __device__ __forceinline__ bool attend_tile(const AttendArgs& a, int64_t r, int nr, int g, float* buf, float* sm,
                                             float* sl) {
     constexpr int NW = kAttendWaves;
-    __shared__ int n_list;
+    __shared__ int listed[NW];
     const KvPages& c = a.c;
     const int G = a.G, tid = threadIdx.x;
     const int lane = tid & 63, w = tid >> 6, col = lane & 15, grp = lane >> 4;
@@ -1075,7 +1077,6 @@ __device__ __forceinline__ bool attend_tile(const AttendArgs& a, int64_t r, int 
     uint32_t* mask = reinterpret_cast<uint32_t*>(buf);               // 16 bits a page: rows that select it
     int32_t* list = reinterpret_cast<int32_t*>(buf) + words;
     for (int i = tid; i < words; i += 64 * NW) mask[i] = 0;
-    if (tid == 0) n_list = 0;
     __syncthreads();
     bool twice = false;
     int last = -1;                                                   // newest position of the tile
@@ -1093,11 +1094,35 @@ __device__ __forceinline__ bool attend_tile(const AttendArgs& a, int64_t r, int 
             const uint32_t bit = 1u << (16 * (idx & 1) + j);
             const uint32_t was = atomicOr(&mask[idx >> 1], bit);
             twice = twice || (was & bit);
-            if (!(was >> (16 * (idx & 1)) & 0xFFFFu)) list[atomicAdd(&n_list, 1)] = idx;
         }
     }
     if (__syncthreads_or(twice)) return false;
-    const int n = n_list;
+    // each wave lists its part of the words, behind those of the waves before it
+    const int seen = min(words, last / (2 * kPage) + 1), part = (seen + 64 * NW - 1) / (64 * NW) * 64;
+    const int end = min((w + 1) * part, seen);
+    int n = 0;
+    for (int i = w * part + lane; i - lane < end; i += 64) {
+        const uint32_t x = i < end ? mask[i] : 0u;
+        n += __popcll(__ballot(x & 0xFFFFu)) + __popcll(__ballot(x >> 16));
+    }
+    if (lane == 0) listed[w] = n;
+    __syncthreads();
+    n = 0;
+    int at = 0;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+        at += v < w ? listed[v] : 0;
+        n += listed[v];
+    }
+    for (int i = w * part + lane; i - lane < end; i += 64) {
+        const uint32_t x = i < end ? mask[i] : 0u;
+        const uint64_t even = __ballot(x & 0xFFFFu), odd = __ballot(x >> 16), below = (1ull << lane) - 1;
+        int k = at + __popcll(even & below) + __popcll(odd & below);
+        if (x & 0xFFFFu) list[k++] = 2 * i;
+        if (x >> 16) list[k] = 2 * i + 1;
+        at += __popcll(even) + __popcll(odd);
+    }
+    __syncthreads();
     const int j = min(col / G, nr - 1), h = col % G;
     const bool mine = col < nr * G;
     const int pos = mine && table_row(a, r + j) ? a.positions[r + j] : -1;

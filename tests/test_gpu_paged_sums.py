@@ -82,3 +82,34 @@ def test_infinite_values(kind):
     assert inf.any() and not np.isnan(ref).any() and np.array_equal(got[inf], ref[inf])
     tol = 1.01 * (e32 + e16 + 2.0**-8 * np.abs(ref))
     assert (np.abs(got[~inf] - ref[~inf]) <= tol[~inf]).all()
+
+
+@pytest.mark.parametrize("hd,G", [(128, 4), (64, 2), (128, 1)])
+def test_calls_repeat_their_bits(hd, G):
+    """Rows that share pages, whose lists name them in any order: the same call
+    again, with other work before it, and with its lists in another order."""
+    n_kv, top_k, lens = 8, 96, [5000, 5000, 5000, 5000]
+    table, slots = scattered(lens, 1300, 320, 5)
+    k, v = fill_pages(table, lens, slots, 1300, n_kv, hd, "bf16")
+    kv = cache_over(table, 1300, n_kv, hd, "bf16", k_pool=k, v_pool=v)
+    n = 440
+    rs = i32(slots[np.arange(n) // 110])
+    pos = i32(4500 + np.arange(n))
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    order = torch.rand((n, n_kv, 280), generator=g, device="cuda").argsort(dim=2).to(torch.int32)
+    sel = order[..., :top_k].contiguous()
+    q = randn((n, n_kv * G, hd), "bf16", 6)
+    lists = [sel, sel.sort(dim=2).values]
+    first = [kv.attend(q, rs, pos, x).view(torch.int16) for x in lists]
+    # rows taken together (16 / G of one slot) read the pages in their order,
+    # single rows in that of their list
+    i = np.arange(n)
+    r0 = i // (16 // G) * (16 // G)
+    together = torch.as_tensor(r0 // 110 == np.minimum(r0 + 16 // G, n) // 110, device="cuda")
+    assert torch.equal(first[0][together], first[1][together])
+    for turn in range(30):
+        if turn % 3 == 1:
+            torch.randn((2000, 2000), device="cuda").sort(dim=0)
+        again = kv.attend(q, rs, pos, lists[turn % 2])
+        assert torch.equal(first[turn % 2], again.view(torch.int16)), turn
