@@ -36,7 +36,10 @@ int outlets::fail(int rc, const std::string& msg) {
 
 namespace {
 
+// The error is reported here, so it does not stay behind in the thread, where a
+// later call's launch check would find it.
 int hip_fail(hipError_t e, const char* what) {
+    (void)hipGetLastError();
     return fail(OUTLETS_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
@@ -184,7 +187,10 @@ struct outlets_ctx {
         if (!spare.empty()) { e = spare.back(); spare.pop_back(); return e; }
         // timing only: no system-scope fence (a cache write-back and
         // invalidate per record would perturb the work being timed)
-        if (hipEventCreateWithFlags(&e, hipEventDisableSystemFence) != hipSuccess) return nullptr;
+        if (hipEventCreateWithFlags(&e, hipEventDisableSystemFence) != hipSuccess) {
+            (void)hipGetLastError();
+            return nullptr;
+        }
         return e;
     }
 
@@ -192,6 +198,7 @@ struct outlets_ctx {
         if (bytes == 0) bytes = 256;
         hipError_t e = hipMalloc(p, bytes);
         if (e != hipSuccess) {
+            (void)hipGetLastError();
             *p = nullptr;
             return fail(OUTLETS_ERR_NOMEM, std::string("hipMalloc of ") + std::to_string(bytes) +
                                                " bytes failed: " + hipGetErrorString(e));
@@ -217,6 +224,15 @@ struct outlets_ctx {
 };
 
 namespace {
+
+// Makes the context's device the current one for a call's launches.  An error
+// that an earlier HIP call of the thread left unread is dropped: the launch
+// checks are about the call's own work.
+int use_device(const outlets_ctx* c) {
+    (void)hipGetLastError();
+    HIP_TRY(hipSetDevice(c->device), "hipSetDevice");
+    return OUTLETS_OK;
+}
 
 // Records an event pair around the launches of one kernel group when
 // profiling is on.
@@ -748,7 +764,7 @@ int predict_step_impl(outlets_ctx* ctx, bool noalloc, int32_t n_req, const int32
     const char* why = "";
     rc = ctx->pager->check_step(n_req, slots, &why);
     if (rc) return fail(rc, why);
-    HIP_TRY(hipSetDevice(ctx->device), "hipSetDevice");
+    if (int err = use_device(ctx)) return err;
     hipStream_t st = static_cast<hipStream_t>(stream);
 
     // the new token's position is each slot's cached length before the append
@@ -1066,7 +1082,7 @@ int outlets_predict_prefill(outlets_ctx* ctx, int32_t n_req, const int32_t* slot
     if (rc) return rc;
     if (hdraft_out && ctx->act_fmt == FMT_BF16 && !aligned16(hdraft_out))
         return fail(OUTLETS_ERR_UNSUPPORTED, "hdraft_out must be 16-byte aligned");
-    HIP_TRY(hipSetDevice(ctx->device), "hipSetDevice");
+    if (int err = use_device(ctx)) return err;
     hipStream_t st = static_cast<hipStream_t>(stream);
 
     std::vector<int32_t> updates;
@@ -1189,7 +1205,7 @@ int outlets_probe_prefill(outlets_ctx* ctx, int32_t n_req, const int32_t* slots,
         T += lens[i];
     }
     if (T > ctx->cfg.max_batch_tokens) return fail(OUTLETS_ERR_INVALID_ARG, "total prompt tokens exceed max_batch_tokens");
-    HIP_TRY(hipSetDevice(ctx->device), "hipSetDevice");
+    if (int err = use_device(ctx)) return err;
     hipStream_t st = static_cast<hipStream_t>(stream);
     // req_off [n+1] | req_slot [n] | cu_tiles [n+1]
     std::vector<int32_t> v(3 * n_req + 2);
@@ -1218,7 +1234,7 @@ int outlets_probe_step(outlets_ctx* ctx, int32_t n_req, const int32_t* slots, co
     if (rc || n_req == 0) return rc;
     for (int i = 0; i < n_req; ++i)
         if (ctx->probe_count[slots[i]] == 0) return fail(OUTLETS_ERR_SLOT_EMPTY, "probe slot not active");
-    HIP_TRY(hipSetDevice(ctx->device), "hipSetDevice");
+    if (int err = use_device(ctx)) return err;
     hipStream_t st = static_cast<hipStream_t>(stream);
     // req_slot [n] | req_start [n] (tokens pooled before this one)
     std::vector<int32_t> v(2 * n_req);
@@ -1258,7 +1274,7 @@ int outlets_draft_distribution(outlets_ctx* ctx, int32_t n_req, float* p_out, vo
     if (!p_out) return fail(OUTLETS_ERR_INVALID_ARG, "null p_out");
     if (ctx->last_in_scratch)
         return fail(OUTLETS_ERR_INVALID_ARG, "the last predict call ran in the static scratch (no-allocation step)");
-    HIP_TRY(hipSetDevice(ctx->device), "hipSetDevice");
+    if (int err = use_device(ctx)) return err;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int V = ctx->cfg.vocab;
     const bool split = ctx->w_fmt != FMT_F32;          // hi rows [0, n), lo rows [n, 2n)
@@ -1359,7 +1375,7 @@ int outlets_get_buffer(outlets_ctx* ctx, int32_t which, void* dst, int64_t nbyte
         which != OUTLETS_BUF_BLOCK_KEYS && which != OUTLETS_BUF_SELECTED)
         return fail(OUTLETS_ERR_INVALID_ARG, "the last predict call ran in the static scratch (no-allocation step)");
     if (!dst || nbytes < size) return fail(OUTLETS_ERR_INVALID_ARG, "destination too small");
-    HIP_TRY(hipSetDevice(ctx->device), "hipSetDevice");
+    if (int err = use_device(ctx)) return err;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (which == OUTLETS_BUF_Q) {
         // queries live in the first n_q*hd columns of the fused qkv rows

@@ -36,11 +36,14 @@ private:
     bool changed_ = false;
 };
 
-// Runs a call's body with its device current; no C++ exception leaves.
+// Runs a call's body with its device current; no C++ exception leaves.  An
+// error that an earlier HIP call of the thread left unread is dropped, so that
+// the check behind the body is about its launches alone.
 template <typename F>
 int guarded(int device, F&& body) noexcept {
     try {
         DeviceGuard dev(device);
+        (void)hipGetLastError();
         if (dev.error() != hipSuccess)
             return fail(OUTLETS_ERR_HIP, std::string("device: ") + hipGetErrorString(dev.error()));
         body();
