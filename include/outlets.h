@@ -286,7 +286,8 @@ int outlets_predict_step_noalloc(outlets_ctx* ctx, int32_t n_req, const int32_t*
  * cached pages have no block keys yet (SLOT_BUSY; turning it off is possible
  * at any time).  Errors, nothing changed: sink < 0, local < 1 or
  * sink + local > top_k (INVALID_ARG); more than 16 query heads per KV head
- * (UNSUPPORTED).  After a failed allocation (NOMEM) it is off.
+ * (UNSUPPORTED).  After a failed allocation (NOMEM) it is off and
+ * holds no memory.
  */
 int outlets_sparse_steps(outlets_ctx* ctx, int32_t top_k, int32_t sink, int32_t local);
 

@@ -1041,8 +1041,11 @@ int outlets_sparse_steps(outlets_ctx* ctx, int32_t top_k, int32_t sink, int32_t 
     HIP_TRY(hipDeviceSynchronize(), "hipDeviceSynchronize");
     ctx->sparse_top = 0;
     ctx->last_sparse = 0;
-    for (void** p : {&ctx->block_keys, &ctx->sparse_ws, &ctx->sparse_rec}) ctx->release(p);
-    ctx->release(&ctx->sparse_sel);
+    const auto free_all = [ctx] {
+        for (void** p : {&ctx->block_keys, &ctx->sparse_ws, &ctx->sparse_rec}) ctx->release(p);
+        ctx->release(&ctx->sparse_sel);
+    };
+    free_all();
     const KvPages c = ctx->pages();
     const int64_t Bm = cfg.max_batch_requests, eb = static_cast<int64_t>(fmt_bytes(ctx->act_fmt));
     // selections of large batches go part by part through 256 MiB of scores
@@ -1055,7 +1058,10 @@ int outlets_sparse_steps(outlets_ctx* ctx, int32_t top_k, int32_t sink, int32_t 
     if (!rc) rc = ctx->alloc(reinterpret_cast<void**>(&ctx->sparse_sel), sizeof(int32_t) * Bm * cfg.n_kv_heads * top_k);
     if (!rc) rc = ctx->alloc(&ctx->sparse_ws, ctx->sparse_ws_bytes);
     if (!rc) rc = ctx->alloc(&ctx->sparse_rec, rec);
-    if (rc) return rc;
+    if (rc) {
+        free_all();
+        return rc;
+    }
     ctx->sparse_sink = sink;
     ctx->sparse_local = local;
     ctx->sparse_top = top_k;

@@ -72,3 +72,15 @@ def test_predict_calls_after_a_failed_allocation():
     a.step(range(3), *device_states(case, step_inputs(case, 1)))
     assert a.buffer("SELECTED", torch.int32).numel() == 3 * 2 * 4
     a.close(), b.close()
+
+
+def test_a_refused_size_holds_no_memory():
+    """What was allocated before the allocation that failed is freed."""
+    case = make_case(1, lens=[100, 60, 127], shape=reduced_shape(), n_req=3)
+    pred = make_predictor(case, max_seq_len=400, max_batch_requests=4096, max_slots=4096, num_pages=200000)
+    torch.cuda.synchronize()
+    free = torch.cuda.mem_get_info()[0]
+    with pytest.raises(B.OutletsError):
+        pred.sparse_steps(2**31 - 1, 1, 4)           # its block keys alone take 102 MB
+    assert torch.cuda.mem_get_info()[0] == free
+    pred.close()
