@@ -51,6 +51,10 @@ def _take(buffers, name, shape, dtype, device, fill=None):
     return t
 
 
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
 def _check_i32(t, name, n, index):
     """Data pointer of a contiguous int32 vector (of n entries) on device `index`."""
     if t.dtype != torch.int32 or t.get_device() != index or t.dim() != 1 or not t.is_contiguous() or \
@@ -88,9 +92,9 @@ class PageTables:
 
     ``buffers`` may hold the caller's own ``free_bits`` (int32
     [ceil(num_pages / 32)]), ``page_table`` (int32 [max_slots,
-    ceil(max_seq_len / 16)]) and ``seq_len`` (int32 [max_slots]); given any, all
-    are taken as they are (``reset`` empties them), otherwise the state starts
-    empty."""
+    ceil(max_seq_len / 16)]) and ``seq_len`` (int32 [max_slots]); given any, the
+    state has only those, as they are (``append``, ``release`` and ``reset``
+    need all three and are refused without), otherwise it starts empty."""
 
     def __init__(self, num_pages: int, max_slots: int, max_seq_len: int, device=0,
                  buffers: Optional[Dict[str, torch.Tensor]] = None):
@@ -99,11 +103,12 @@ class PageTables:
         self._index = self.device.index
         self.num_pages, self.max_slots, self.max_seq_len = num_pages, max_slots, max_seq_len
         self.max_pages = -(-max_seq_len // PAGE)
-        self.free_bits = _take(buffers, "free_bits", (-(-num_pages // 32),), torch.int32, self.device)
-        self.page_table = _take(buffers, "page_table", (max_slots, self.max_pages), torch.int32, self.device)
-        self.seq_len = _take(buffers, "seq_len", (max_slots,), torch.int32, self.device)
-        self._c = B.outlets_page_state(self.free_bits.data_ptr(), self.page_table.data_ptr(), self.seq_len.data_ptr(),
-                                       num_pages, max_slots, max_seq_len, self.device.index)
+        shapes = dict(free_bits=(-(-num_pages // 32),), page_table=(max_slots, self.max_pages), seq_len=(max_slots,))
+        got = {name: _take(buffers, name, shape, torch.int32, self.device)
+               if not buffers or buffers.get(name) is not None else None for name, shape in shapes.items()}
+        self.free_bits, self.page_table, self.seq_len = got["free_bits"], got["page_table"], got["seq_len"]
+        self._c = B.outlets_page_state(_ptr(self.free_bits), _ptr(self.page_table), _ptr(self.seq_len), num_pages,
+                                       max_slots, max_seq_len, self.device.index)
         self._ref = C.byref(self._c)
         if not buffers:
             self.reset()
@@ -166,10 +171,9 @@ class PagedKV:
         got = {name: _take(buffers, name, shape, self.dtype, self.device) if not buffers or name in buffers else None
                for name, shape in shapes.items()}
         self.k_pool, self.v_pool, self.block_keys = got["k_pool"], got["v_pool"], got["block_keys"]
-        ptr = {name: None if t is None else t.data_ptr() for name, t in got.items()}
-        self._c = B.outlets_kv_pages(ptr["k_pool"], ptr["v_pool"], ptr["block_keys"], tables.page_table.data_ptr(),
-                                     _FMT[fmt], n_kv, head_dim, p, tables.max_slots, tables.max_pages,
-                                     self.device.index)
+        self._c = B.outlets_kv_pages(_ptr(self.k_pool), _ptr(self.v_pool), _ptr(self.block_keys),
+                                     _ptr(tables.page_table), _FMT[fmt], n_kv, head_dim, p, tables.max_slots,
+                                     tables.max_pages, self.device.index)
         self._ref = C.byref(self._c)
 
     def _heads(self, t, name, n, heads):
