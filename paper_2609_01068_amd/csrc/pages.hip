@@ -306,10 +306,10 @@ template <bool STREAM> __device__ __forceinline__ void put16(void* p, u32x4 x) {
 // registers to their rows; values, and keys for the block keys, cross LDS,
 // where a wave takes a run.  The keys of a page that a
 // run completes are in LDS (this call's) or in the pool (earlier calls'), so
-// its block key needs no second pass.
+// its block key needs no second pass.  The launch's tiles start at row `first`.
 template <typename T, int HD, int TR, bool VEC>
 __global__ void __launch_bounds__(256)
-cache_write(KvPages c, int n_rows, const int32_t* __restrict__ slot_map, const T* __restrict__ k, int64_t ldk,
+cache_write(KvPages c, int64_t first, int n_rows, const int32_t* __restrict__ slot_map, const T* __restrict__ k, int64_t ldk,
             const T* __restrict__ v, int64_t ldv) {
     constexpr int EX = TR + kPage - 1;              // the last run may end behind the tile
     constexpr bool STREAM = TR > 16;
@@ -325,12 +325,13 @@ cache_write(KvPages c, int n_rows, const int32_t* __restrict__ slot_map, const T
     __shared__ int runs[TR], n_runs;
     // the heads of a tile on one XCD (blocks i and i + 8 share one): rows of
     // k and v stand far apart, so one head's parts meet on few L2 channels
-    const int y = blockIdx.x / 8, g = y % c.n_kv, r0 = (y / c.n_kv * 8 + blockIdx.x % 8) * TR, tid = threadIdx.x;
+    const int y = blockIdx.x / 8, g = y % c.n_kv, tid = threadIdx.x;
+    const int64_t r0 = first + (y / c.n_kv * 8 + blockIdx.x % 8) * TR;
     if (r0 >= n_rows) return;
     const int limit = c.num_pages * kPage;
     if (tid == 0) n_runs = 0;
     for (int i = tid; i <= EX; i += 256) {
-        const int r = r0 - 1 + i;
+        const int64_t r = r0 - 1 + i;
         const int s = r >= 0 && r < n_rows ? slot_map[r] : -1;
         sm[i] = s >= 0 && s < limit ? s : -1;
     }
@@ -346,7 +347,7 @@ cache_write(KvPages c, int n_rows, const int32_t* __restrict__ slot_map, const T
         own[i] = sm[i + 1] >= 0 && j >= 0 && j < TR;
     }
     __syncthreads();
-    const int rows = min(EX, n_rows - r0);
+    const int rows = static_cast<int>(min<int64_t>(EX, n_rows - r0));
     for (int e = tid; e < rows * (HD / VE); e += 256) {
         const int i = e / (HD / VE), ch = e % (HD / VE) * VE, s = sm[i + 1];
         if (!own[i]) continue;
@@ -401,6 +402,10 @@ cache_write(KvPages c, int n_rows, const int32_t* __restrict__ slot_map, const T
     }
 }
 
+// Workgroups of one launch; more go out in several (the threads of a grid's
+// axis are counted in 32 bits).
+constexpr int64_t kWriteBlocks = 1 << 20;
+
 template <typename T>
 void write_rows(const KvPages& c, int n_rows, const int32_t* slot_map, const void* k, int64_t ldk, const void* v,
                 int64_t ldv, hipStream_t st) {
@@ -410,8 +415,13 @@ void write_rows(const KvPages& c, int n_rows, const int32_t* slot_map, const voi
                      (ldk * sizeof(T)) % 16 == 0 && (ldv * sizeof(T)) % 16 == 0;
     const bool big = n_rows >= kBigWrite && sizeof(T) == 2;
 #define OUTLETS_WRITE(HD, TR, VEC)                                                                             \
-    hipLaunchKernelGGL((cache_write<T, HD, TR, VEC>), dim3((n_rows + 8 * TR - 1) / (8 * TR) * 8 * c.n_kv), dim3(256), 0, st, c, \
-                       n_rows, slot_map, kk, ldk, vv, ldv)
+    do {                                                                                                       \
+        const int64_t row = 8 * static_cast<int64_t>(c.n_kv), per = std::max<int64_t>(1, kWriteBlocks / row);  \
+        const int64_t tiles = (static_cast<int64_t>(n_rows) + 8 * TR - 1) / (8 * TR);    /* eight of them */   \
+        for (int64_t t = 0; t < tiles; t += per)                                                               \
+            hipLaunchKernelGGL((cache_write<T, HD, TR, VEC>), dim3(std::min(per, tiles - t) * row), dim3(256), 0, st, c, \
+                               t * (8 * TR), n_rows, slot_map, kk, ldk, vv, ldv);                              \
+    } while (0)
     if (c.hd == 128) {
         if (!vec) OUTLETS_WRITE(128, 16, false);
         else if (big) OUTLETS_WRITE(128, (sizeof(T) == 2 ? 32 : 16), true);

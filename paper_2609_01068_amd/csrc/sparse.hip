@@ -1306,8 +1306,11 @@ void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int
     const int slices = both ? std::min(24, score_slices(c)) : score_slices(c);
     const int cap = plain ? c.max_pages : fused || both ? kFusedPages : -1;
     const int ld = score_stride(c), lds_row = std::min(ld, kFusedPages);
-    const int slab = static_cast<int>(std::min<int64_t>(plain ? rows.n_rows : ws_bytes / row_bytes,
-                                                        std::min(rows.n_rows, 32768)));     // (the grid's z)
+    // rows of one launch: the grid's z, and the threads of its x, which are
+    // counted in 32 bits (fused form: 256 a row and KV head)
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(32768, (1 << 23) / c.n_kv));
+    const int slab = static_cast<int>(
+        std::min<int64_t>(plain ? rows.n_rows : ws_bytes / row_bytes, std::min<int64_t>(rows.n_rows, most)));
     int tile = plain ? 1 : 16 / gp;
     if (fused || both)
         while (tile > 1 && tile * lds_row * 4 > kFusedBytes) tile /= 2;
