@@ -279,8 +279,9 @@ __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__bf16 x) { return static_cast<float>(x); }
 
 // The mean of a page's keys of one channel: the 64-bit sum of 16 stored
-// values (exact unless their exponents are more than 40 apart), rounded to
-// 32 bits and then to the storage format.
+// values in position order (exact where their exponents are at most 41 apart in
+// bf16, 25 in fp32: 8 or 24 significant bits, and 4 for the sum, in 53), rounded
+// to 32 bits and then to the storage format.
 template <typename T> __device__ __forceinline__ T block_mean(double sum) {
     return static_cast<T>(static_cast<float>(sum * (1.0 / kPage)));
 }

@@ -35,10 +35,16 @@ __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_ex
 // Selection is made of comparisons of s_b = max over the group's heads of
 // q_h . kbar_b, and its result is defined by the 64-bit scores.  They are not
 // computed for every page: scores in 32 bits (matrix instructions for bf16)
-// come with a bound on their error, and only pages closer to the border than
-// that bound are scored again in 64 bits.  The first pass is then bound by
-// reading the block keys; in the 512-row step (normal keys and queries, 260
-// candidate pages, 59 wanted) one row in nine scores two pages again.
+// come with a bound on their error, one for all pages scored together.  A
+// histogram of 256 equal bins between a row's extremes gives the border's bin.
+// Where some page of that bin is closer to the border than the bound, all of the
+// bin are scored again in 64 bits, or, past near_cap of them, all of it at once,
+// through memory.  The first pass is then bound by reading the block keys: in the
+// 512-row step (normal keys and queries, 260 candidate pages, 59 wanted) one row
+// in nine scores two pages again.  Scores far from all others widen the bins:
+// with one page at 30, 100 and 300 standard deviations of a request's scores
+// the step takes 65, 185 and 392 us instead of 53, 445 prompt rows of 1,650
+// pages 68, 301 and 570 instead of 61.
 //
 // Error of a 32-bit score: sums of at most 128 products, each step off by at
 // most 2^-23 of the partial sum's magnitude, hence by 2^-16 sum |q k|; 2^-14
@@ -1297,7 +1303,10 @@ void launch_block_select(const KvPages& c, const BlockRows& rows, int top_k, int
     // Long tables and many rows, more or less one of each slot (a decode step):
     // the rows whose caches are short take the fused form all the same
     // (8 heads of 512 rows of 264 pages at the mean, in tables of 2,048 and 8,192:
-    // 90 and 158 us by the split form alone, 74 and 102 by both).
+    // 90 and 158 us by the split form alone, 74 and 102 by both).  Few prompts'
+    // rows beside many slots take it too, and find nothing in the fused form (445
+    // rows of 4 of 512 slots: 66 us in tables of 2,049 pages, where 6 slots take
+    // 64; 114 us in tables of 8,192).
     const bool both =
         !fused && rows.n_rows < 2 * c.max_slots && static_cast<int64_t>(rows.n_rows) * c.n_kv >= 4 * cus;
     // many rows are waves enough: fewer blocks for those with nothing to score
@@ -1388,7 +1397,8 @@ void launch_block_attention(const KvPages& c, const BlockRows& rows, const int32
     const int splits = attend_splits(static_cast<int64_t>(rows.n_rows) * c.n_kv, top_k, cus);
     const int64_t eb = c.fmt == OUTLETS_FMT_F32 ? 4 : 2;
     // rows taken together: as many as fill the 16 columns and whose page list
-    // and masks fit the LDS that their states need
+    // and masks fit the LDS that their states need (445 prompt rows, 4 together
+    // in tables of up to 8,192 pages: 109 us; one by one in tables of 16,384: 244)
     int tile = c.fmt == OUTLETS_FMT_F32 || splits > 1 ? 1 : 16 / G;
     while (tile > 1 && 4 * ((c.max_pages + 1) / 2 + static_cast<int64_t>(tile) * top_k) > kTileBytes) tile /= 2;
     for (int r0 = 0; r0 < rows.n_rows; r0 += kAttendRows) {
