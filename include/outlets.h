@@ -31,6 +31,8 @@
  * return an int status: OUTLETS_OK (0) or a negative OUTLETS_ERR_* code.
  * No C++ exception crosses this boundary.  outlets_last_error() gives a
  * message for the calling thread's last failure.
+ * A call that launches work drops a HIP error that an earlier HIP call of the
+ * thread left unread; it reports its own launches only.
  *
  * Memory ownership: the caller owns every buffer passed in (weights,
  * activations, outputs); weights registered by outlets_create must stay
